@@ -211,7 +211,7 @@ def _project(H, Wq, w_scale, sums):
     x = H.double()
     top = x.abs().amax(1, keepdim=True)
     q = torch.where(top > 0, torch.round(x * 127.0 / top), torch.zeros_like(x))
-    s = top.float() / 127.0
+    s = (top / 127.0).float()     # (a quotient by a number is a product with its reciprocal on the GPU: in 64 bits, too)
     acc = q.to(sums) @ Wq[:, :H.shape[1]].to(sums).T
     return acc.float() * s * w_scale
 
