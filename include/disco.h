@@ -45,6 +45,8 @@ extern "C" {
 #define DISCO_TOPK 10                 /* k of Top_k in Eq. 2 (footnote: k = 10 in all experiments) */
 #define DISCO_NFEAT (DISCO_TOPK + 2)  /* top-k probabilities, entropy, position */
 #define DISCO_MAX_CLF_HIDDEN 256
+#define DISCO_MAX_BEAMS 64            /* beams of a sequence */
+#define DISCO_MAX_KEPT 128            /* continuations kept of a sequence */
 
 enum {
     DISCO_OK = 0,
@@ -56,6 +58,9 @@ enum {
                                          context's counters are then undefined: destroy it */
     DISCO_ERR_STATIC_LIMIT = -6       /* size beyond the fixed scratch of disco_draft_step_static */
 };
+
+/* Types of hidden states and logits where a call takes more than one. */
+enum { DISCO_F32 = 0, DISCO_BF16 = 1, DISCO_F16 = 2 };
 
 typedef struct disco_ctx disco_ctx;
 
@@ -359,6 +364,82 @@ int disco_iteration_host(disco_ctx* ctx, const void* W_D /*device*/, size_t w_st
                          const int32_t* sl_forced_host, const int32_t* draft_ids_host,
                          int32_t* token_host, float* conf_host, uint8_t* halt_host, int32_t* sl_host,
                          int32_t* n_accept_host, int32_t* bonus_host, int32_t* pos_next_host, void* stream);
+
+/*
+ * ---- LM head in 8-bit integers, beam search ----
+ * The paper has no counterpart.  A decoder is bound by reading its LM head, and an 8-bit head is half as long; beams are the other
+ * use that a draft model's logits are put to.  The calls below need the context's device to be the current one (otherwise
+ * DISCO_ERR_INVALID_ARG), take at most max(max_batch, max_rows) rows (DISCO_ERR_WORKSPACE), and read nothing ahead of the
+ * work before them in the stream: a head may be quantised right before it is used.
+ */
+
+/*
+ * Rows to 8-bit integers with a scale each (symmetric, no zero point): a head once, row by row; hidden rows by the calls below.
+ *     scale[r] = max_k |x[r, k]| / 127,      q[r, k] = rint(127 x[r, k] / max_k |x[r, k]|)
+ * The quotient is rounded to the nearest integer as it is (ties to even), never as an intermediate rounding makes it.  A row of zeros
+ * has scale 0; a row with a number that is not finite has scale NaN and q = 0.
+ *   x      x_type [rows, d], rows ldx elements apart (ldx >= d, a multiple of 16 bytes); 16-byte aligned; d a multiple of 8, up to 16384
+ *   q      int8 [rows, ldq], 16-byte aligned; ldq >= d, a multiple of 16.  Columns d .. are written up to the next multiple of 16, as zeros
+ *   scale  float [rows]
+ */
+int disco_quantize_rows(disco_ctx* ctx, const void* x, int x_type, long long ldx, int rows, int d, int8_t* q,
+                        long long ldq, float* scale, void* stream);
+
+/*
+ * Logits of R hidden rows by an 8-bit LM head:
+ *     y[r, v] = (float)(sum_k q_h[r, k] W_q[v, k]) * s_h[r] * w_scale[v]
+ * with q_h and s_h the hidden rows quantised as above, integer sums, and both products rounded to fp32 (y to its own type at
+ * the end).  A hidden row that holds a number that is not finite gives a row of NaN.
+ *   W_q      int8 [V, ldw]  (ldw >= d, a multiple of 16; what lies behind column d is not read), w_scale float [V]
+ *   H        h_type [R, d], rows ldh elements apart, as x above; d at most the larger of the context's widths
+ *   y        y_type [R, V], rows ldy >= V elements apart (any alignment of its type); what lies behind column V is left as it is
+ */
+int disco_project_int8(disco_ctx* ctx, const int8_t* W_q, long long ldw, const float* w_scale, const void* H, int h_type,
+                       long long ldh, int d, int R, void* y, int y_type, long long ldy, void* stream);
+
+/*
+ * One step of beam search for B sequences of K beams: of all continuations of a sequence the n best by
+ *     l[k, v] = score[k] + logits[k, v] - ln sum_w exp(logits[k, w]),
+ * best first.  Equal ones: the lower beam, then the lower token.  (A beam's continuations are ordered by their logits; scores of different
+ * beams are compared in 64 bits.)
+ *   logits    z_type [B * K, V], rows ldz >= V elements apart (any alignment of its type).  -inf is a token that is not allowed
+ *   score     float [B, K]   sums of log-probabilities; a beam at -inf (or NaN, +inf) is dead: it has no continuation and its
+ *             logits are not read.  (At the first token all beams but one are.)
+ *   finished  uint8 [B, K] or NULL   non-zero: the beam has ended; its one continuation is (score, eos), its logits are not read
+ *   eos       the token that ends a sequence, or -1 if there is none (then finished must be NULL)
+ * A row with a NaN or +inf, or with nothing but -inf, is no distribution and has no continuation.
+ * Outputs:
+ *   score_out [B, n], parent [B, n] (the beam), token [B, n]; finished_out uint8 [B, n] or NULL: the parent had ended, or token == eos.
+ *   Places that no continuation is left for get (-inf, -1, -1, 0).  With n == K, score_out may be score and finished_out finished.
+ * 1 <= K <= DISCO_MAX_BEAMS, 1 <= n <= DISCO_MAX_KEPT.
+ */
+int disco_beam_select(disco_ctx* ctx, const void* logits, int z_type, long long ldz, int B, int K, const float* score,
+                      const uint8_t* finished, int eos, int n, float* score_out, int32_t* parent, int32_t* token,
+                      uint8_t* finished_out, void* stream);
+
+/*
+ * disco_project_int8 and disco_beam_select in one call, with the soft-max statistics taken while the logits are made.
+ *   H      h_type [B * K, d]; W_q, ldw, w_scale, ldh as in disco_project_int8; the other arguments as in disco_beam_select
+ *   work   float [B * K, V], 16-byte aligned: the call's work space; what it holds afterwards is not specified
+ */
+int disco_beam_step_int8(disco_ctx* ctx, const int8_t* W_q, long long ldw, const float* w_scale, const void* H, int h_type,
+                         long long ldh, int d, int B, int K, const float* score, const uint8_t* finished, int eos, int n,
+                         float* score_out, int32_t* parent, int32_t* token, uint8_t* finished_out, float* work,
+                         void* stream);
+
+/*
+ * Beam states (caches, token histories) to where their beams' children are:
+ *     dst[i][b * n + j, m, t, :] = src[i][b * K + parent[b, j], m, t, :]      0 <= m < mid, 0 <= t < lens[b] (T without lens)
+ *   src, dst    HOST arrays of `tensors` device pointers: contiguous [B * K, mid, T, unit_bytes] and [B * n, mid, T, unit_bytes]
+ *               (a cache [beam, head, position, width]: mid = heads; [beam, position, ...]: mid = 1)
+ *   parent      int32 [B, n]; -1: the child's rows are left as they are; otherwise outside [0, K): the same, and DISCO_ERR_INVALID_ARG
+ *               in the device status word
+ *   lens        int32 [B] or NULL: positions in use; those behind are left as they are (outside [0, T]: the nearer end)
+ * All tensors in place (dst[i] == src[i], n == K; only rows that change are written) or none; other overlaps are refused.
+ */
+int disco_beam_reorder(disco_ctx* ctx, const void* const* src, void* const* dst, int tensors, int B, int K, int n,
+                       const int32_t* parent, const int32_t* lens, long long mid, long long T, long long unit_bytes,
+                       void* stream);
 
 /*
  * Draft step without any allocation.  (The paper has no counterpart: this is a packaging variant of

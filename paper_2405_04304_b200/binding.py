@@ -7,6 +7,7 @@ and streams only); the ``*_host`` calls take CPU tensors (pinned for asynchronou
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -32,7 +33,11 @@ EXPORTS = [
     "disco_draft_step_host", "disco_verify_ragged_host", "disco_draft_step_static", "disco_draft_step_ppl",
     "disco_draft_step_sample", "disco_verify_sample_ragged", "disco_extract_features",
     "disco_draft_loop", "disco_verify_sl", "disco_iteration", "disco_iteration_host", "disco_test_hooks",
+    "disco_quantize_rows", "disco_project_int8", "disco_beam_select", "disco_beam_step_int8", "disco_beam_reorder",
 ]
+
+MAX_BEAMS = 64
+MAX_KEPT = 128
 
 
 class DiscoError(RuntimeError):
@@ -88,6 +93,11 @@ def load() -> ctypes.CDLL:
                                     vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.disco_iteration_host.argtypes = [vp, vp, sz, vp, vp, vp, ci, vp, ctypes.POINTER(_Clf), cf, ci, vp, vp,
                                          vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.disco_quantize_rows.argtypes = [vp, vp, ci, ll, ci, ci, vp, ll, vp, vp]
+    lib.disco_project_int8.argtypes = [vp, vp, ll, vp, vp, ci, ll, ci, ci, vp, ci, ll, vp]
+    lib.disco_beam_select.argtypes = [vp, vp, ci, ll, ci, ci, vp, vp, ci, ci, vp, vp, vp, vp, vp]
+    lib.disco_beam_step_int8.argtypes = [vp, vp, ll, vp, vp, ci, ll, ci, ci, ci, vp, vp, ci, ci, vp, vp, vp, vp, vp, vp]
+    lib.disco_beam_reorder.argtypes = [vp, vp, vp, ci, ci, ci, ci, vp, vp, ll, ll, ll, vp]
     _lib = lib
     return lib
 
@@ -121,6 +131,15 @@ def _stream(stream) -> int:
     if _raw_stream is not None and _get_device is not None:
         return _raw_stream(_get_device())
     return torch.cuda.current_stream().cuda_stream
+
+
+# Types that disco.h has numbers for.
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def int8_pitch(d: int) -> int:
+    """Bytes from row to row of an 8-bit head of width d: the next multiple of 16."""
+    return (int(d) + 15) // 16 * 16
 
 
 class Classifier:
@@ -169,6 +188,7 @@ class Context:
             self._h = ctypes.c_void_p()
             raise DiscoError(rc, "disco_create")
         self.V, self.d_draft, self.d_target = V, d_draft, d_target
+        self.device = torch.cuda.current_device()
         self.max_batch, self.max_rows = max_batch, max_rows
 
     def close(self):
@@ -333,6 +353,140 @@ class Context:
             h(pos_next, torch.int32), _stream(stream))
         if rc != OK:
             raise DiscoError(rc, "disco_iteration_host")
+
+    # ---------------------------------------------------------------- 8-bit LM head, beam search
+    def _on(self, t, dtype):
+        """Address of a contiguous tensor of the context's device (None -> NULL)."""
+        if t is not None and t.get_device() != self.device:
+            raise ValueError(f"expected a tensor on cuda:{self.device}, the context's device")
+        return _ptr(t, dtype)
+
+    def _rows(self, t, width: int):
+        """(address, type number, elements from row to row) of a matrix [..., width] whose rows may lie apart."""
+        code = _TYPES.get(t.dtype)
+        if code is None:
+            raise TypeError(f"expected float32, bfloat16 or float16, got {t.dtype}")
+        if t.get_device() != self.device:
+            raise ValueError(f"expected a tensor on cuda:{self.device}, the context's device")
+        if t.dim() < 2 or t.shape[-1] != width:
+            raise ValueError(f"expected rows of {width}, got shape {tuple(t.shape)}")
+        if t.is_contiguous():
+            return t.data_ptr(), code, width
+        if t.dim() != 2 or t.stride(1) != 1 or t.stride(0) < width:
+            raise ValueError("rows must be contiguous and must not overlap")
+        return t.data_ptr(), code, t.stride(0)
+
+    def _head(self, W_q, w_scale):
+        if W_q.dim() != 2 or W_q.shape[0] != self.V or w_scale.numel() != self.V:
+            raise ValueError(f"expected an 8-bit head of {self.V} rows with a scale each")
+        return self._on(W_q, torch.int8), int(W_q.shape[1]), self._on(w_scale, torch.float32)
+
+    def _beams(self, score, score_out, parent, token, finished, finished_out):
+        """(B, K, n) after a look at the shapes."""
+        if score.dim() != 2 or score_out.dim() != 2 or score_out.shape[0] != score.shape[0]:
+            raise ValueError("score must be [B, K] and score_out [B, n]")
+        if parent.shape != score_out.shape or token.shape != score_out.shape:
+            raise ValueError("parent and token must have the shape of score_out")
+        if (finished is not None and finished.shape != score.shape) or \
+                (finished_out is not None and finished_out.shape != score_out.shape):
+            raise ValueError("finished must have the shape of score, finished_out that of score_out")
+        return score.shape[0], score.shape[1], score_out.shape[1]
+
+    def _here(self, stream) -> int:
+        if stream is not None:
+            return stream.cuda_stream
+        if _raw_stream is not None:
+            return _raw_stream(self.device)
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def quantize_rows(self, X, Q, scale, stream=None) -> None:
+        """disco_quantize_rows: X [rows, d] (float32, bfloat16, float16) to Q int8 [rows, int8_pitch(d) or more] and scale [rows]."""
+        rows, d = X.shape
+        x, code, ldx = self._rows(X, d)
+        if Q.dim() != 2 or Q.shape[0] != rows or Q.shape[1] < int8_pitch(d) or scale.numel() != rows:
+            raise ValueError(f"expected Q [{rows}, {int8_pitch(d)} or more] and {rows} scales")
+        rc = self._lib.disco_quantize_rows(self._h, x, code, ldx, rows, d, self._on(Q, torch.int8), int(Q.shape[1]),
+                                           self._on(scale, torch.float32), self._here(stream))
+        if rc != OK:
+            raise DiscoError(rc, "disco_quantize_rows")
+
+    def project_int8(self, W_q, w_scale, H, y, stream=None) -> None:
+        """disco_project_int8: logits y [R, V] of hidden rows H [R, d] by the 8-bit head W_q [V, ldw], w_scale [V]."""
+        w, ldw, ws = self._head(W_q, w_scale)
+        R, d = H.shape
+        h, h_type, ldh = self._rows(H, d)
+        out, y_type, ldy = self._rows(y, self.V)
+        if y.dim() != 2 or y.shape[0] != R:
+            raise ValueError(f"expected y [{R}, {self.V}]")
+        rc = self._lib.disco_project_int8(self._h, w, ldw, ws, h, h_type, ldh, d, R, out, y_type, ldy, self._here(stream))
+        if rc != OK:
+            raise DiscoError(rc, "disco_project_int8")
+
+    def beam_select(self, logits, score, score_out, parent, token, finished=None, eos: int = -1, finished_out=None,
+                    stream=None) -> None:
+        """disco_beam_select: logits [B * K, V] or [B, K, V], score [B, K]; score_out, parent, token, finished_out [B, n]."""
+        B, K, n = self._beams(score, score_out, parent, token, finished, finished_out)
+        z, z_type, ldz = self._rows(logits, self.V)
+        if logits.numel() != B * K * self.V:
+            raise ValueError(f"expected logits of {B * K} rows")
+        rc = self._lib.disco_beam_select(
+            self._h, z, z_type, ldz, B, K, self._on(score, torch.float32), self._on(finished, torch.uint8), int(eos), n,
+            self._on(score_out, torch.float32), self._on(parent, torch.int32), self._on(token, torch.int32),
+            self._on(finished_out, torch.uint8), self._here(stream))
+        if rc != OK:
+            raise DiscoError(rc, "disco_beam_select")
+
+    def beam_step_int8(self, W_q, w_scale, H, score, score_out, parent, token, work, finished=None, eos: int = -1,
+                       finished_out=None, stream=None) -> None:
+        """disco_beam_step_int8: hidden rows H [B * K, d] through the 8-bit head to the n best continuations of each sequence;
+        work float32 [B * K, V] (or as many numbers) is the call's work space."""
+        B, K, n = self._beams(score, score_out, parent, token, finished, finished_out)
+        w, ldw, ws = self._head(W_q, w_scale)
+        if H.dim() != 2 or H.shape[0] != B * K:
+            raise ValueError(f"expected H [{B * K}, d]")
+        d = H.shape[1]
+        h, h_type, ldh = self._rows(H, d)
+        if work.numel() < B * K * self.V:
+            raise ValueError(f"expected work of {B * K} x {self.V} numbers")
+        rc = self._lib.disco_beam_step_int8(
+            self._h, w, ldw, ws, h, h_type, ldh, d, B, K, self._on(score, torch.float32), self._on(finished, torch.uint8),
+            int(eos), n, self._on(score_out, torch.float32), self._on(parent, torch.int32), self._on(token, torch.int32),
+            self._on(finished_out, torch.uint8), self._on(work, torch.float32), self._here(stream))
+        if rc != OK:
+            raise DiscoError(rc, "disco_beam_step_int8")
+
+    def beam_reorder(self, src, dst, parent, lens=None, length_dim: int = 1, stream=None) -> None:
+        """disco_beam_reorder: lists of states [B * K, ...] to [B * n, ...] by parent [B, n]; dst may be src (n == K).
+
+        lens [B]: positions in use, along dimension length_dim of the states (what lies behind them is left as it is)."""
+        if len(src) == 0 or len(src) != len(dst) or parent.dim() != 2:
+            raise ValueError("expected as many states in dst as in src, and parent [B, n]")
+        B, n = parent.shape
+        shape, dtype = tuple(src[0].shape), src[0].dtype
+        rows = shape[0]
+        if B == 0 or rows == 0 or rows % B or not 1 <= length_dim <= len(shape):
+            raise ValueError(f"{rows} rows are no beams of {B} sequences, or there is no dimension {length_dim}")
+        inner = shape[1:]
+        if lens is not None and (length_dim == len(shape) or lens.numel() != B):
+            raise ValueError(f"expected {B} lengths along one of the states' dimensions")
+        want = (B * n,) + inner
+        ends = shape, want
+        count = len(src)
+        ptrs = []
+        for states, expected in zip((src, dst), ends):
+            for t in states:
+                if t.shape != expected or t.dtype != dtype or t.get_device() != self.device or not t.is_contiguous():
+                    raise ValueError(f"expected contiguous {dtype} states {expected} on cuda:{self.device}, got {t.dtype} {tuple(t.shape)}")
+                ptrs.append(t.data_ptr())
+        mid = math.prod(inner[:length_dim - 1])
+        T = inner[length_dim - 1] if length_dim <= len(inner) else 1
+        unit = math.prod(inner[length_dim:]) * src[0].element_size()
+        array = ctypes.c_void_p * count
+        rc = self._lib.disco_beam_reorder(
+            self._h, array(*ptrs[:count]), array(*ptrs[count:]), count, B, rows // B, n, self._on(parent, torch.int32),
+            self._on(lens, torch.int32), mid, T, unit, self._here(stream))
+        if rc != OK:
+            raise DiscoError(rc, "disco_beam_reorder")
 
     # ---------------------------------------------------------------- host-buffer calls
     def draft_step_host(self, W_D, h_D, pos, n_drafted, clf: Classifier, tau: float, sl_max: int,

@@ -13,6 +13,7 @@ constexpr int kTopK = DISCO_TOPK;
 constexpr int kNFeat = DISCO_NFEAT;
 constexpr unsigned kFullMask = 0xffffffffu;
 constexpr int kNoIndex = 0x7fffffff;
+constexpr int kI8Chunk = 32;   // vocabulary rows per record of soft-max statistics that the 8-bit LM head leaves
 
 // Bounded-wait budget: a wait gives up after this many clock ticks (about 0.05 s by default).  A device
 // variable, one copy per translation unit, so that a test can shorten it (disco_test_hooks) and make a wait

@@ -10,6 +10,7 @@
 #include <new>
 
 #include "disco.h"
+#include "context.cuh"
 #include "stream_tail.cuh"
 #include "umma_tail.cuh"
 #include "draft_batch.cuh"
@@ -23,24 +24,14 @@ using namespace disco;
 namespace {
 
 constexpr int kStreamWarps = 16;     // consumer warps of the streaming kernel
-constexpr int kMaxHidden = 16384;    // widest hidden dimension the kernels accept
 constexpr int kSlotTargetBytes = 6144;
 
-constexpr int kMaxDevices = 64;
+
 // Hidden states that disco_iteration_host has a kernel bring over rather than the copy engine: by then the engine's second copy,
 // which runs beside the draft phase, has made up for what its first one and the events around it cost (us per call, 32000 x 768
 // and a target of the width given, engine -> kernel: 37 KB 69.0 -> 65.0, 150 KB 107.6 -> 104.4, 230 KB 108.1 -> 106.0, 256 KB 106.6 ->
 // 104.0, 420 KB 106.7 -> 109.5, 490 KB 84.4 -> 86.5).
 constexpr size_t kFetchBytes = 288 * 1024;
-
-// One-time, per-device configuration of one kernel (its dynamic shared-memory limit).  Every template
-// instance of a launcher owns one of these; the lock makes first calls from several host threads, and
-// contexts on several devices, safe.
-struct KernelSetup {
-    std::mutex mu;
-    bool done[kMaxDevices] = {};
-    size_t dyn_limit[kMaxDevices] = {};
-};
 
 // Where an LM-head pass leaves its records (m, Z first) of consecutive vocabulary slabs: what a draw is located with.
 struct RecordLayout {
@@ -54,90 +45,6 @@ struct StreamPlan {
     size_t smem;
     bool ok;
 };
-
-}  // namespace
-
-struct disco_ctx {
-    int device;
-    int V, d_draft, d_target, max_batch, max_rows, clf_hidden;
-    int sm_count;
-    size_t smem_optin;
-    int path;
-    int pdl;  // launch the streaming kernel with programmatic stream serialization (DISCO_PDL=0 turns it off)
-    long long launches;
-    cudaStream_t last_stream;  // stream of the most recent enqueue (disco_last_device_status waits for it only)
-    unsigned int test_stamp_skew;  // disco_test_hooks
-    void* device_mem;  // every device buffer below
-    void* host_mem;    // the pinned staging below
-    // scratch for cross-block reductions
-    int part_rows;  // rows the partial buffers can hold
-    int max_grid;
-    unsigned long long* keys;
-    unsigned int* ticket;
-    int* status;
-    float* final_stats;            // [part_rows][2] (m, Z) of the rows of a pass
-    float* final_stats2;           // the same for the second pass of a feature extraction
-    uint8_t* chain_alive;          // [max_batch] draft phase on the device: which sequences still draft
-    double* sample_seg_tot;        // verification with sampling: [max_batch][kSampleMaxSegments][2] sums of weights
-    int32_t* sample_seg_last;      //   the same shape: last index with positive weight
-    unsigned int* sample_tickets;  //   [max_batch]
-    void* pack_rows;               // fixed-shape verification with many rows: the rows that count, packed
-    int32_t* pack_off;             // [max(max_batch, max_rows) + 1] their offsets; the last entry is the row count
-    void* loop_rec;                // persistent draft-phase kernel: stamped 80-byte records, [4][CTA]; written by nothing else
-    void* part_rec;                // draft step: 64-byte partial records, [sequence][CTA]
-    void* stamped_rec;             // batched draft step: stamped 80-byte records, [sequence][CTA]; written by nothing else
-    unsigned int* row_bound;       // batched draft step: two sets of [part_rows][kDbBoundStride] words, see DraftBatchParams
-    int part_slots;                // partials per row the buffers can hold
-    void* encode_tiled;            // cuTensorMapEncodeTiled, resolved through the runtime
-    void* pointer_attributes;      // cuPointerGetAttributes, the same way
-    // device staging for the *_host entry points
-    void* stage_hidden;
-    void* stage_hidden_draft;      // disco_iteration_host: the draft hidden states of all steps
-    int32_t* stage_dev;            // disco_iteration_host: pos0 | sl_forced (max_batch each) | draft_ids (max_rows)
-    cudaStream_t copy_stream;      // disco_iteration_host: the target hidden states travel beside the draft phase
-    cudaEvent_t copy_done;
-    // Small inputs and outputs of the *_host entry points live in pinned host memory that the GPU maps:
-    // the kernels read and write it in place, so a host call costs one copy (the hidden states), one
-    // launch and one synchronisation.  *_h: host address, *_d: the same memory as the device sees it.
-    int32_t *stage_int_h, *stage_int_d;    // pos | n_drafted | token | draft_ids | row_off | n_accept | bonus | target_ids
-    float *stage_float_h, *stage_float_d;  // conf | feats
-    uint8_t *stage_byte_h, *stage_byte_d;  // active | halt
-};
-
-namespace {
-
-// With DISCO_DEBUG set in the environment, failed CUDA runtime calls are reported on stderr.
-inline bool cuda_ok(cudaError_t e, const char* what) {
-    if (e == cudaSuccess) return true;
-    static const bool verbose = std::getenv("DISCO_DEBUG") != nullptr;
-    if (verbose) std::fprintf(stderr, "[disco] %s: %s\n", what, cudaGetErrorString(e));
-    return false;
-}
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// Raise a kernel's dynamic shared-memory limit once per device: to `bytes`, or (bytes == 0) to all that the
-// device allows beside the kernel's static shared memory.  *limit receives the value in force.
-template <typename Kern>
-bool raise_smem_limit(const disco_ctx* c, KernelSetup& ks, Kern kern, size_t bytes, size_t* limit) {
-    if (c->device < 0 || c->device >= kMaxDevices) return false;
-    std::lock_guard<std::mutex> lock(ks.mu);
-    if (!ks.done[c->device]) {
-        size_t want = bytes;
-        if (want == 0) {
-            cudaFuncAttributes fa;
-            if (!cuda_ok(cudaFuncGetAttributes(&fa, kern), "cudaFuncGetAttributes")) return false;
-            want = c->smem_optin - fa.sharedSizeBytes;
-        }
-        if (!cuda_ok(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)want),
-                     "cudaFuncSetAttribute"))
-            return false;
-        ks.dyn_limit[c->device] = want;
-        ks.done[c->device] = true;
-    }
-    if (limit) *limit = ks.dyn_limit[c->device];
-    return true;
-}
 
 StreamPlan plan_stream(const disco_ctx* c, int V, int d, int RT, int clf_H) {
     StreamPlan pl{};
@@ -212,10 +119,6 @@ int run_stream(disco_ctx* c, TailParams& p, int clf_H, cudaStream_t st) {
 // ------------------------------------------------------------------------------------------------
 // tcgen05 path
 // ------------------------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // bf16 [rows, d] row-major, boxes of box_rows x 64 elements, 128-byte swizzle, zero fill out of bounds
 bool encode_bf16_2d(const disco_ctx* c, CUtensorMap* map, const void* base, int rows, int d, int box_rows) {
     if (!c->encode_tiled) return false;
@@ -630,7 +533,7 @@ int disco_create(disco_ctx** out, int V, int d_draft, int d_target, int max_batc
         void** p;
         size_t at;
     };
-    Piece pieces[32];
+    Piece pieces[40];
     int n_pieces = 0;
     auto device = [&](auto** p, size_t bytes) {
         pieces[n_pieces++] = Piece{reinterpret_cast<void**>(p), dev_bytes};
@@ -643,6 +546,7 @@ int disco_create(disco_ctx** out, int V, int d_draft, int d_target, int max_batc
     // R rows take R * (sm_count / ceil(R / 128)) <= 128 * sm_count records
     device(&c->stamped_rec, (size_t)128 * c->sm_count * 80);       // no stamp yet
     device(&c->row_bound, (size_t)2 * c->part_rows * kDbBoundStride * 4);
+    device(&c->beam_tickets, (size_t)c->part_rows * sizeof(unsigned int));
     zero_bytes = dev_bytes;
     device(&c->part_rec, slots * 64);
     device(&c->final_stats, (size_t)c->part_rows * 2 * sizeof(float));
@@ -657,6 +561,13 @@ int disco_create(disco_ctx** out, int V, int d_draft, int d_target, int max_batc
     device(&c->stage_hidden, hid);
     device(&c->stage_hidden_draft, (size_t)max_rows * d_draft * 2);
     device(&c->stage_dev, (2 * (size_t)max_batch + (size_t)max_rows) * sizeof(int32_t));
+    c->int8_pitch = (std::max(d_draft, d_target) + 15) & ~15;
+    device(&c->int8_rows, (size_t)c->part_rows * c->int8_pitch);
+    device(&c->int8_scale, ((size_t)c->part_rows + 64) * sizeof(float));   // (read in fours)
+    device(&c->beam_stats, (size_t)c->part_rows * ((V + (size_t)kI8Chunk - 1) / kI8Chunk) * sizeof(float2));
+    device(&c->beam_score, (size_t)c->part_rows * DISCO_MAX_KEPT * sizeof(double));
+    device(&c->beam_token, (size_t)c->part_rows * DISCO_MAX_KEPT * sizeof(int32_t));
+    device(&c->beam_count, (size_t)c->part_rows * sizeof(int32_t));
     auto pinned = [&](size_t bytes) {
         const size_t at = host_bytes;
         host_bytes += (bytes + 255) & ~(size_t)255;
@@ -720,6 +631,7 @@ int disco_test_hooks(disco_ctx* c, long long wait_budget_clocks, int withhold_re
     if (!c || wait_budget_clocks < 0) return DISCO_ERR_INVALID_ARG;
     const long long budget = wait_budget_clocks ? wait_budget_clocks : kDefaultWaitBudgetClocks;
     if (cudaMemcpyToSymbol(g_wait_budget_clocks, &budget, sizeof(budget)) != cudaSuccess) return DISCO_ERR_CUDA;
+    if (set_beam_wait_budget(budget) != DISCO_OK) return DISCO_ERR_CUDA;
     c->test_stamp_skew = withhold_records ? 0x40000000u : 0u;
     return DISCO_OK;
 }
@@ -733,24 +645,6 @@ int disco_set_kernel_path(disco_ctx* c, int which) {
 }  // extern "C"
 
 namespace {
-// Launch a small follow-up kernel with programmatic stream serialization (it waits with griddepcontrol.wait
-// before it reads anything), so that its launch latency hides behind the kernel before it.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_after(const disco_ctx* c, void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                         Args... args) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = c->pdl ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
-}
-
 // Host memory as the device sees it, if all of [p, p + bytes) is pinned, 16-byte aligned memory of one allocation.
 const void* device_view(const disco_ctx* c, const void* p, size_t bytes) {
     if (!c->pointer_attributes || !aligned16(p)) return nullptr;

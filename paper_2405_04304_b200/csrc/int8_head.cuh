@@ -1,0 +1,419 @@
+// An LM head in 8-bit integers, with a scale for each hidden row and each vocabulary row:
+//
+//   s_x[r] = max_k |x[r, k]| / 127,   q_x[r, k] = rint(127 x[r, k] / max_k |x[r, k]|)
+//   y[r, v] = (sum_k q_x[r, k] q_w[v, k]) * s_x[r] * s_w[v]
+//
+// The sums are exact in 32-bit integers (at most 127 * 127 * 16384 = 2.6e8); a logit sees three roundings to fp32, in this order:
+// the sum, times s_x, times s_w.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "umma_ptx.cuh"
+
+namespace disco {
+
+// ---------------------------------------------------------------------------------------------
+// rows to 8 bits
+// ---------------------------------------------------------------------------------------------
+constexpr int kQuantThreads = 128;
+constexpr int kQuantMaxWidth = 16384;
+
+// 127 x / top to the nearest integer, ties to even, with 0 < top < inf, |x| <= top.  The product with the reciprocal is off by less
+// than 127 * 2^-22; only where it comes nearer to the middle between two integers than that is the quotient itself needed.
+//   * bf16 and fp16: 127/128 x is exact (7 + 11 bits).  The quotient by `top` is correctly rounded, hence never on the other side
+//     of a tie (2k + 1) / 256, and it is on the tie only if the exact one is: 254 x and (2k + 1) top are multiples of the last place
+//     of x, at most 254 * 2^11 of them, so they differ by 2^-19 of their size or not at all.
+//   * fp32: the same in 64 bits (127 x is exact there, and 254 * 2^24 is well below 2^53).
+template <typename T>
+__device__ __forceinline__ int quantize_one(float x, float top, float inv) {
+    const float p = x * inv;
+    const float r = rintf(p);
+    if (fabsf(p - r) < 0.4995f) return static_cast<int>(r);
+    if constexpr (sizeof(T) == 2) return __float2int_rn(__fdiv_rn(x * 0.9921875f, top) * 128.f);
+    else return __double2int_rn(__ddiv_rn(127.0 * static_cast<double>(x), static_cast<double>(top)));
+}
+
+// Eight consecutive numbers of a row.  (Not by the read-only path: the compiler may move such loads ahead of the wait for the kernel
+// that wrote them.)
+template <typename T>
+struct QuantChunk;
+template <>
+struct QuantChunk<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcg(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void get(float (&f)[8]) const { unpack_bf16x8(v, f); }
+};
+template <>
+struct QuantChunk<__half> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __half* p) { v = __ldcg(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            f[2 * i] = t.x;
+            f[2 * i + 1] = t.y;
+        }
+    }
+};
+template <>
+struct QuantChunk<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = __ldcg(reinterpret_cast<const float4*>(p));
+        b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
+    }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w;
+        f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+    }
+};
+
+struct QuantParams {
+    const void* x;
+    long long ldx;    // elements
+    int d;            // a multiple of 8
+    int8_t* q;
+    long long ldq;    // a multiple of 16; columns d .. round_up(d, 16) - 1 are written as zeros
+    float* scale;
+};
+
+// A CTA to a row; a thread keeps its share of the row (chunks of eight numbers, up to CH of them) in registers between the search
+// for the largest number and the rounding, so that the row is read once.  A row that holds a number that is not finite gets the
+// scale NaN.
+template <typename T, int CH>
+__global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const QuantParams p) {
+    __shared__ uint32_t s_top[kQuantThreads / 32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (only now: what comes next may read the head ahead of its own wait, and the head may be what ran before this)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const long long row = blockIdx.x;
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    const int chunks = p.d >> 3;
+    QuantChunk<T> c[CH];
+    uint32_t top_bits = 0u;     // the order of |x| is that of its bits, and what is not finite comes above all else
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int at = i * kQuantThreads + threadIdx.x;
+        if (at < chunks) {
+            c[i].load(x + 8 * at);
+            float f[8];
+            c[i].get(f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top_bits = max(top_bits, __float_as_uint(f[j]) & 0x7fffffffu);
+        }
+    }
+    top_bits = __reduce_max_sync(kFullMask, top_bits);
+    if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top_bits;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kQuantThreads / 32; ++i) top_bits = max(top_bits, s_top[i]);
+    const bool finite = top_bits < 0x7f800000u;
+    float top = __uint_as_float(top_bits);
+    if (threadIdx.x == 0) p.scale[row] = finite ? __fdiv_rn(top, 127.f) : __uint_as_float(0x7fc00000u);
+    // numbers near the smallest ones are shifted up, which is exact
+    const float shift = top < 0x1p-60f ? 0x1p100f : 1.f;
+    top *= shift;
+    const bool some = finite && top > 0.f;
+    const float inv = some ? 127.f / top : 0.f;
+    int8_t* q = p.q + row * p.ldq;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int at = i * kQuantThreads + threadIdx.x;
+        if (at < chunks) {
+            float f[8];
+            c[i].get(f);
+            uint32_t w[2] = {0u, 0u};
+            if (some) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    w[j >> 2] |= (static_cast<uint32_t>(quantize_one<T>(f[j] * shift, top, inv)) & 0xffu) << (8 * (j & 3));
+            }
+            *reinterpret_cast<uint2*>(q + 8 * at) = make_uint2(w[0], w[1]);
+        }
+    }
+    if ((p.d & 15) && threadIdx.x == 0) *reinterpret_cast<uint2*>(q + p.d) = make_uint2(0u, 0u);
+}
+
+// ---------------------------------------------------------------------------------------------
+// the product
+// ---------------------------------------------------------------------------------------------
+constexpr int kI8BK = 128;                // k elements per stage (one 128-byte swizzle span)
+constexpr int kI8MaxStages = 24;
+constexpr int kI8EpiWarps = 8;
+constexpr int kI8Threads = (2 + kI8EpiWarps) * 32;
+constexpr int kI8FixedSmem = 1024 /*align*/ + 512 /*barriers*/;
+
+__host__ __device__ inline int round_up(int x, int to) { return (x + to - 1) / to * to; }
+
+// How V vocabulary rows and R hidden rows are cut: MT tiles of NT hidden rows (the columns of an accumulator; the MMA takes N of
+// them) times NV tiles of TR vocabulary rows (one or two blocks of 128 TMEM lanes).  Item i is hidden tile i % MT of vocabulary tile
+// i / MT; the CTAs take items in turn, so those that share a vocabulary tile run side by side and the head crosses HBM once.
+struct Int8Tiling {
+    int MT, NT, N, NV, TR, blocks, cols, bufs;
+    __host__ __device__ static Int8Tiling make(int R, int V, int grid, bool whole_chunks) {
+        Int8Tiling t;
+        t.MT = (R + 255) / 256;
+        t.N = round_up((R + t.MT - 1) / t.MT, 16);
+        t.NT = t.N;
+        t.MT = (R + t.NT - 1) / t.NT;
+        // as few rounds of items as tiles of 256 vocabulary rows need, all items alike
+        const long long items = (long long)t.MT * ((V + 255) / 256);
+        const long long rounds = (items + grid - 1) / grid;
+        const long long most = rounds * grid / t.MT;
+        const int nv = (int)(most < V ? (most > 1 ? most : 1) : V);
+        t.TR = (V + nv - 1) / nv;
+        if (whole_chunks) t.TR = round_up(t.TR, kI8Chunk);
+        if (t.TR > 256) t.TR = 256;
+        t.NV = (V + t.TR - 1) / t.TR;
+        t.blocks = t.TR > 128 ? 2 : 1;
+        t.cols = round_up(t.N, 32);
+        t.bufs = 2 * t.blocks * t.cols <= 512 ? 2 : 1;
+        return t;
+    }
+};
+
+// Shared memory of the operand stages: `stages` boxes of vocabulary rows, then as many of hidden rows.  An MMA reads all 128 rows of
+// a block and all N hidden rows: what lies behind the boxes (always inside the ring) only feeds accumulators that nobody reads.
+struct Int8Ring {
+    int stages, w_bytes, x_bytes, bytes;
+    __host__ __device__ static int size(const Int8Ring& r, const Int8Tiling& t, int stages) {
+        const int all = stages * (r.w_bytes + r.x_bytes), last = (stages - 1) * r.w_bytes + t.blocks * 128 * kI8BK;
+        return round_up(all > last ? all : last, 1024);
+    }
+    // As many stages as fit `limit` bytes; none if that is less than two.
+    __host__ __device__ static Int8Ring make(const Int8Tiling& t, long long limit) {
+        Int8Ring r{};
+        r.w_bytes = round_up(t.TR * kI8BK, 1024);
+        r.x_bytes = t.N * kI8BK;
+        int stages = kI8MaxStages;
+        while (stages >= 2 && kI8FixedSmem + size(r, t, stages) > limit) --stages;
+        if (stages >= 2) r.stages = stages, r.bytes = size(r, t, stages);
+        return r;
+    }
+};
+
+struct Int8Params {
+    int V, d, R;
+    Int8Tiling t;
+    Int8Ring ring;
+    int x_box;                 // rows of the hidden-row box (a multiple of 8, <= N)
+    const float* w_scale;      // [V]
+    const float* x_scale;      // [R], 16-byte aligned, with room behind for 32 more
+    void* y;
+    long long ldy;
+    float2* stats;             // [R][chunks] (largest logit of the chunk, sum of exp(z - largest)), or null
+    int chunks;
+    int* status;
+};
+
+__device__ __forceinline__ void tc_mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Instruction descriptor: signed 8-bit x signed 8-bit -> signed 32-bit, both operands K-major, M = m, N = n.
+__device__ __forceinline__ uint32_t umma_idesc_i8(int n, uint32_t m = 128) {
+    return (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | ((m >> 4) << 24);
+}
+// The largest of a warp's numbers, NaN if one of them is.
+__device__ __forceinline__ float warp_max_nan_f32(float x) {
+    float m;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
+    return m;
+}
+
+__device__ __forceinline__ void store_logit(float* p, float z) { *p = z; }
+__device__ __forceinline__ void store_logit(__nv_bfloat16* p, float z) { *p = __float2bfloat16_rn(z); }
+__device__ __forceinline__ void store_logit(__half* p, float z) { *p = __float2half_rn(z); }
+
+// Soft-max statistics of 32 logits of one hidden row, one per lane: the largest (NaN if there is one that is not a number) and the
+// sum of exp(z - largest).  The sum is taken in units of 2^-26, as integers: one instruction, no order of summation, off by at most
+// 2^-27 a term where the largest term is 1.
+__device__ __forceinline__ float2 warp_chunk_stats(float z) {
+    const float m = warp_max_nan_f32(z);
+    const uint32_t e = m > DISCO_NEG_INF && m < -DISCO_NEG_INF ? __float2uint_rn(__expf(z - m) * 0x1p26f) : 0u;
+    return make_float2(m, static_cast<float>(__reduce_add_sync(kFullMask, e)) * 0x1p-26f);
+}
+
+// Vocabulary rows on the TMEM lanes, hidden rows on the columns: a warp's 32 results of a column are neighbours in y, so they go
+// from registers to memory in whole lines, and the head, which is what HBM has to deliver, is cut as finely as there are SMs.
+//   * warp 0    producer: a box of TR vocabulary rows x 128 k and one of the tile's hidden rows per stage
+//   * warp 1    MMA issuer: M = 128 (twice for more than 128 vocabulary rows), N = hidden rows of the tile, K = 32
+//   * warps 2+  epilogue: a thread owns a vocabulary row and walks over the hidden rows
+template <typename Out, bool STATS>
+__global__ void __launch_bounds__(kI8Threads, 1)
+int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_constant__ CUtensorMap tmap_X, const Int8Params p) {
+    extern __shared__ uint8_t smem_dyn[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
+    uint8_t* w_tiles = smem;
+    uint8_t* x_tiles = smem + p.ring.stages * p.ring.w_bytes;
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + p.ring.bytes);
+    uint64_t* empty = full + kI8MaxStages;
+    uint64_t* tmem_full = empty + kI8MaxStages;
+    uint64_t* tmem_empty = tmem_full + 2;
+    uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(tmem_empty + 2);
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const Int8Tiling& t = p.t;
+    const int KB = (p.d + kI8BK - 1) / kI8BK;
+    const int items = t.MT * t.NV;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.ring.stages; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&tmem_full[b], 1);
+            mbar_init(&tmem_empty[b], kI8EpiWarps);
+        }
+        fence_mbar_init();
+        prefetch_tensormap(&tmap_W);
+        prefetch_tensormap(&tmap_X);
+    }
+    if (warp == 1) {
+        tmem_alloc(tmem_base_s, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_base_s;
+
+    if (warp == 0) {
+        // ------------------------------ producer ------------------------------
+        if (elect_one()) {
+            const uint32_t full0 = smem_addr(full), empty0 = smem_addr(empty), w0 = smem_addr(w_tiles), x0 = smem_addr(x_tiles);
+            const uint32_t expected = (uint32_t)(t.TR + p.x_box) * 128u;
+            const int k_end = KB * kI8BK;
+            int item = blockIdx.x;
+            // The head is complete before the kernel that rounds the hidden rows lets this one start: its first tiles are
+            // requested at once, the hidden rows of the same stages behind the wait for that kernel.
+            const int pre = item < items ? min(p.ring.stages, KB) : 0;
+            for (int n = 0; n < pre; ++n) {
+                mbar_arrive_expect_tx(full0 + n * 8, expected);
+                tma_load_2d(w0 + n * p.ring.w_bytes, &tmap_W, n * kI8BK, item / t.MT * t.TR, full0 + n * 8);
+            }
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+            for (int n = 0; n < pre; ++n)
+                tma_load_2d(x0 + n * p.ring.x_bytes, &tmap_X, n * kI8BK, item % t.MT * t.NT, full0 + n * 8);
+            int stage = pre == p.ring.stages ? 0 : pre, phase = pre == p.ring.stages ? 1 : 0;
+            int k = pre * kI8BK;
+            for (; item < items; item += gridDim.x, k = 0) {
+                const int v0 = item / t.MT * t.TR, r0 = item % t.MT * t.NT;
+                for (; k < k_end; k += kI8BK) {
+                    const uint32_t bar = full0 + stage * 8;
+                    mbar_wait(empty0 + stage * 8, phase ^ 1, p.status);
+                    mbar_arrive_expect_tx(bar, expected);
+                    tma_load_2d(w0 + stage * p.ring.w_bytes, &tmap_W, k, v0, bar);
+                    tma_load_2d(x0 + stage * p.ring.x_bytes, &tmap_X, k, r0, bar);
+                    if (++stage == p.ring.stages) stage = 0, phase ^= 1;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------ MMA issuer ------------------------------
+        if (elect_one()) {
+            const uint32_t idesc = umma_idesc_i8(t.N);
+            const uint32_t full0 = smem_addr(full), empty0 = smem_addr(empty);
+            const uint64_t w_desc0 = umma_smem_desc(w_tiles), x_desc0 = umma_smem_desc(x_tiles);
+            const uint32_t w_step = (uint32_t)p.ring.w_bytes >> 4, x_step = (uint32_t)p.ring.x_bytes >> 4;   // descriptor units
+            uint64_t w_desc = w_desc0, x_desc = x_desc0;
+            int stage = 0, phase = 0, it = 0;
+            for (int item = blockIdx.x; item < items; item += gridDim.x, ++it) {
+                const int b = t.bufs == 2 ? it & 1 : 0;
+                mbar_wait(&tmem_empty[b], ((t.bufs == 2 ? it >> 1 : it) & 1) ^ 1, p.status);
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + b * t.blocks * t.cols;
+                for (int kb = 0; kb < KB; ++kb) {
+                    mbar_wait(full0 + stage * 8, phase, p.status);
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)       // 32 k elements = 32 bytes = 2 descriptor units
+                        tc_mma_i8(d_tmem, w_desc + 2 * k, x_desc + 2 * k, idesc, (kb | k) != 0);
+                    if (t.blocks == 2) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)   // 128 vocabulary rows further on
+                            tc_mma_i8(d_tmem + t.cols, w_desc + (128 * 128 >> 4) + 2 * k, x_desc + 2 * k, idesc, (kb | k) != 0);
+                    }
+                    tc_commit(empty0 + stage * 8);
+                    w_desc += w_step;
+                    x_desc += x_step;
+                    if (++stage == p.ring.stages) stage = 0, phase ^= 1, w_desc = w_desc0, x_desc = x_desc0;
+                }
+                tc_commit(&tmem_full[b]);
+            }
+        }
+    } else {
+        // ------------------------------ epilogue ------------------------------
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        const int quad = warp & 3;             // TMEM lane quadrant this warp may read
+        const int block = (warp - 2) >> 2;     // block of 128 vocabulary rows
+        const int tile_row = block * 128 + quad * 32;
+        int it = 0;
+        for (int item = blockIdx.x; item < items; item += gridDim.x, ++it) {
+            const int b = t.bufs == 2 ? it & 1 : 0;
+            const int vt = item / t.MT, v0 = vt * t.TR, r0 = item % t.MT * t.NT;
+            const int vocab = min(t.TR, p.V - v0), rows = min(t.NT, p.R - r0);
+            const int v = v0 + tile_row + lane;
+            const bool in = tile_row + lane < vocab;
+            const float ws = in ? __ldcg(p.w_scale + v) : 0.f;
+            mbar_wait(&tmem_full[b], (t.bufs == 2 ? it >> 1 : it) & 1, p.status);
+            tc_fence_after();
+            if (tile_row < vocab) {
+                const uint32_t tmem = tmem_base + (b * t.blocks + block) * t.cols + (static_cast<uint32_t>(quad * 32) << 16);
+                Out* y = static_cast<Out*>(p.y) + (long long)r0 * p.ldy + v;
+                float2* stats = STATS ? p.stats + (long long)r0 * p.chunks + vt * (t.TR / kI8Chunk) + tile_row / kI8Chunk : nullptr;
+#pragma unroll 1
+                for (int c = 0; c < rows; c += 32) {
+                    float xs[32];      // (r0 + c is a multiple of 16)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 q = *reinterpret_cast<const float4*>(p.x_scale + r0 + c + 4 * i);
+                        xs[4 * i] = q.x, xs[4 * i + 1] = q.y, xs[4 * i + 2] = q.z, xs[4 * i + 3] = q.w;
+                    }
+                    float acc[32];
+                    tmem_ld32(tmem + c, acc);
+                    float2 mine = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        if (c + i < rows) {
+                            const float z = __fmul_rn(__fmul_rn(static_cast<float>(__float_as_int(acc[i])), xs[i]), ws);
+                            if (in) store_logit(y, z);
+                            y += p.ldy;
+                            if constexpr (STATS) {
+                                const float2 s = warp_chunk_stats(in ? z : DISCO_NEG_INF);
+                                if (lane == i) mine = s;
+                            }
+                        }
+                    }
+                    if constexpr (STATS) {
+                        if (c + lane < rows) stats[(long long)(c + lane) * p.chunks] = mine;
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tmem_empty[b]);
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 512);
+    }
+}
+
+}  // namespace disco

@@ -1,0 +1,67 @@
+"""Host-only checks of the 8-bit LM head's tiling (compiled from the kernels' own header, run on the CPU), and of what the beam-search entry
+points refuse before they touch a GPU."""
+import ctypes
+import os
+import subprocess
+
+from paper_2405_04304_b200 import binding, build
+
+_TILING = r"""
+#include "int8_head.cuh"
+#include <cstdio>
+using namespace disco;
+int main() {
+    const int grids[] = {1, 3, 147, 148}, vs[] = {1, 31, 128, 129, 300, 4000, 32000, 40011, 49152, 151936};
+    for (int grid : grids)
+        for (int V : vs)
+            for (int R = 1; R < 5000; R += R < 600 ? 1 : 61)
+                for (int chunks = 0; chunks < 2; ++chunks) {
+                    const Int8Tiling t = Int8Tiling::make(R, V, grid, chunks);
+                    bool ok = t.NT >= 1 && t.N >= t.NT && t.N % 16 == 0 && t.N <= 256 && (long long)t.MT * t.NT >= R && (long long)(t.MT - 1) * t.NT < R;
+                    ok = ok && t.TR >= 1 && t.TR <= 256 && t.TR <= 128 * t.blocks && (long long)t.NV * t.TR >= V && (long long)(t.NV - 1) * t.TR < V;
+                    ok = ok && (!chunks || t.TR % kI8Chunk == 0);
+                    // accumulators of all buffers, as columns of tensor memory; reads of 32 columns end inside theirs
+                    ok = ok && t.bufs * t.blocks * t.cols <= 512 && t.cols >= t.N && t.cols % 32 == 0 && t.NT % 16 == 0;
+                    const Int8Ring r = Int8Ring::make(t, 227 * 1024);
+                    ok = ok && r.stages >= 2 && r.stages <= kI8MaxStages && kI8FixedSmem + r.bytes <= 227 * 1024;
+                    ok = ok && r.w_bytes % 1024 == 0 && r.x_bytes % 1024 == 0 && r.w_bytes >= t.TR * kI8BK;
+                    // what the last stage's MMAs read
+                    ok = ok && (r.stages - 1) * r.w_bytes + t.blocks * 128 * kI8BK <= r.bytes && r.stages * (r.w_bytes + r.x_bytes) <= r.bytes;
+                    // no more rounds of items than whole tiles of 256 need
+                    const long long whole = (long long)t.MT * ((V + 255) / 256);
+                    ok = ok && ((long long)t.MT * t.NV + grid - 1) / grid <= (whole + grid - 1) / grid;
+                    if (!ok) return std::printf("R %d V %d grid %d chunks %d\n", R, V, grid, chunks), 1;
+                }
+    return 0;
+}
+"""
+
+
+def _run(tmp_path, source):
+    src, exe = tmp_path / "rules.cu", tmp_path / "rules"
+    src.write_text(source)
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    subprocess.run([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-I", build.CSRC, "-I", include, "-o", str(exe),
+                    str(src)], check=True)
+    run = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert run.returncode == 0, (run.returncode, run.stdout)
+
+
+def test_int8_tiling_covers_everything_and_stays_in_its_memory(tmp_path):
+    _run(tmp_path, _TILING)
+
+
+def test_null_contexts_are_refused():
+    build.build()
+    lib = binding.load()
+    z = ctypes.c_void_p(None)
+    assert lib.disco_quantize_rows(None, z, 0, 8, 1, 8, z, 16, z, z) == binding.ERR_INVALID_ARG
+    assert lib.disco_project_int8(None, z, 16, z, z, 1, 8, 8, 1, z, 0, 1, z) == binding.ERR_INVALID_ARG
+    assert lib.disco_beam_select(None, z, 0, 1, 1, 1, z, z, -1, 1, z, z, z, z, z) == binding.ERR_INVALID_ARG
+    assert lib.disco_beam_step_int8(None, z, 16, z, z, 1, 8, 8, 1, 1, z, z, -1, 1, z, z, z, z, z, z) == binding.ERR_INVALID_ARG
+    assert lib.disco_beam_reorder(None, z, z, 1, 1, 1, 1, z, z, 1, 1, 1, z) == binding.ERR_INVALID_ARG
+
+
+def test_int8_pitch():
+    assert [binding.int8_pitch(d) for d in (8, 16, 24, 768, 1000)] == [16, 16, 32, 768, 1008]
