@@ -357,9 +357,15 @@ class Context:
     # ---------------------------------------------------------------- 8-bit LM head, beam search
     def _on(self, t, dtype):
         """Address of a contiguous tensor of the context's device (None -> NULL)."""
-        if t is not None and t.get_device() != self.device:
+        if t is None:
+            return None
+        if t.dtype is dtype and t.get_device() == self.device and t.is_contiguous():
+            return t.data_ptr()
+        if t.dtype is not dtype:
+            raise TypeError(f"expected {dtype}, got {t.dtype}")
+        if t.get_device() != self.device:
             raise ValueError(f"expected a tensor on cuda:{self.device}, the context's device")
-        return _ptr(t, dtype)
+        raise ValueError("tensor must be contiguous")
 
     def _rows(self, t, width: int):
         """(address, type number, elements from row to row) of a matrix [..., width] whose rows may lie apart."""
@@ -368,7 +374,7 @@ class Context:
             raise TypeError(f"expected float32, bfloat16 or float16, got {t.dtype}")
         if t.get_device() != self.device:
             raise ValueError(f"expected a tensor on cuda:{self.device}, the context's device")
-        if t.dim() < 2 or t.shape[-1] != width:
+        if t.dim() < 2 or t.size(-1) != width:
             raise ValueError(f"expected rows of {width}, got shape {tuple(t.shape)}")
         if t.is_contiguous():
             return t.data_ptr(), code, width
@@ -383,14 +389,14 @@ class Context:
 
     def _beams(self, score, score_out, parent, token, finished, finished_out):
         """(B, K, n) after a look at the shapes."""
-        if score.dim() != 2 or score_out.dim() != 2 or score_out.shape[0] != score.shape[0]:
+        beams, kept = score.shape, score_out.shape
+        if len(beams) != 2 or len(kept) != 2 or kept[0] != beams[0]:
             raise ValueError("score must be [B, K] and score_out [B, n]")
-        if parent.shape != score_out.shape or token.shape != score_out.shape:
+        if parent.shape != kept or token.shape != kept:
             raise ValueError("parent and token must have the shape of score_out")
-        if (finished is not None and finished.shape != score.shape) or \
-                (finished_out is not None and finished_out.shape != score_out.shape):
+        if (finished is not None and finished.shape != beams) or (finished_out is not None and finished_out.shape != kept):
             raise ValueError("finished must have the shape of score, finished_out that of score_out")
-        return score.shape[0], score.shape[1], score_out.shape[1]
+        return beams[0], beams[1], kept[1]
 
     def _here(self, stream) -> int:
         if stream is not None:
@@ -459,24 +465,21 @@ class Context:
         """disco_beam_reorder: lists of states [B * K, ...] to [B * n, ...] by parent [B, n]; dst may be src (n == K).
 
         lens [B]: positions in use, along dimension length_dim of the states (what lies behind them is left as it is)."""
-        if len(src) == 0 or len(src) != len(dst) or parent.dim() != 2:
+        count = len(src)
+        if count == 0 or count != len(dst) or parent.dim() != 2:
             raise ValueError("expected as many states in dst as in src, and parent [B, n]")
         B, n = parent.shape
-        shape, dtype = tuple(src[0].shape), src[0].dtype
-        rows = shape[0]
+        shape, dtype, device = src[0].shape, src[0].dtype, self.device
+        rows, inner = shape[0], shape[1:]
         if B == 0 or rows == 0 or rows % B or not 1 <= length_dim <= len(shape):
             raise ValueError(f"{rows} rows are no beams of {B} sequences, or there is no dimension {length_dim}")
-        inner = shape[1:]
         if lens is not None and (length_dim == len(shape) or lens.numel() != B):
             raise ValueError(f"expected {B} lengths along one of the states' dimensions")
-        want = (B * n,) + inner
-        ends = shape, want
-        count = len(src)
         ptrs = []
-        for states, expected in zip((src, dst), ends):
+        for states, expected in ((src, shape), (dst, torch.Size((B * n,) + inner))):
             for t in states:
-                if t.shape != expected or t.dtype != dtype or t.get_device() != self.device or not t.is_contiguous():
-                    raise ValueError(f"expected contiguous {dtype} states {expected} on cuda:{self.device}, got {t.dtype} {tuple(t.shape)}")
+                if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.shape != expected:
+                    raise ValueError(f"expected contiguous {dtype} states {tuple(expected)} on cuda:{device}, got {t.dtype} {tuple(t.shape)}")
                 ptrs.append(t.data_ptr())
         mid = math.prod(inner[:length_dim - 1])
         T = inner[length_dim - 1] if length_dim <= len(inner) else 1

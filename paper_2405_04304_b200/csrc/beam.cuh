@@ -3,10 +3,10 @@
 // Selection.  Of a sequence with K beams of score c_k and logits z_k[v], the n best continuations by
 //     l[k, v] = c_k + z_k[v] - ln sum_w exp z_k[w],      ties to the lowest (k, v).
 // Every logit is read once, by a pass that leaves two numbers for each chunk of neighbouring logits: the largest, and the sum of
-// exp(z - largest).  (The 8-bit LM head's epilogue leaves the same.)  What follows looks at few logits: the n best of a row lie in the
-// n chunks that come first by (largest logit, lowest index), since each of those holds a candidate that beats whatever lies in
-// another chunk.  A row's n best then meet those of the sequence's other beams.  Scores are formed and compared in 64 bits: which of two
-// candidates is the better is a whole number, and the scores of different beams may come as near to each other as they like.
+// exp(z - largest).  (The 8-bit LM head's epilogue leaves the same.)  What follows looks at few logits: the n best lie in the n chunks
+// that come first by (best score, place), since each of those holds a candidate that beats whatever lies in
+// another chunk.  Scores are formed and compared in 64 bits: which of two candidates is the better is a whole number, and the scores of
+// different beams may come as near to each other as they like.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -20,12 +20,35 @@ namespace disco {
 constexpr int kBeamChunk = 128;          // logits to a chunk of the pass over given logits
 constexpr int kBeamWarpChunks = 8;       // chunks that a warp takes, so that 32 loads are on their way at once
 constexpr int kBeamStatWarps = 8;
-constexpr int kBeamThreads = 256;        // of the selection
+constexpr int kBeamThreads = 1024;       // of the selection, at most
+constexpr int kBeamItems = 8;            // pieces of rows that a thread of it holds
 constexpr int kBeamMaxKept = DISCO_MAX_KEPT;
 constexpr int kBeamMaxBeams = DISCO_MAX_BEAMS;
-constexpr int kBeamList = 512;           // candidates that are ranked by counting
-constexpr int kBeamChunkList = 2 * kBeamMaxKept + 8;
-constexpr int kBeamSmemKeys = 8192;      // chunks of a row whose keys are held in shared memory
+constexpr int kBeamList = 1024;          // candidates that are ranked by counting
+constexpr int kBeamPieceList = 512;      // pieces that are looked into
+
+// How the chunks of a sequence's K rows are dealt to the warps of its CTA: a lane holds the largest logits of kBeamItems pieces, each of
+// `merged` neighbouring chunks of one row.  Up to as many beams as warps: `share` warps to a row; up to twice as many (of 32 warps): two
+// rows to a warp, half the pieces each.
+struct BeamDeal {
+    int two, share, merged, pieces, used;   // pieces of a row; how many of a lane's items there are, of a row
+    __host__ __device__ static BeamDeal make(int K, int chunks, int warps) {
+        BeamDeal d;
+        d.two = K > warps;
+        d.share = d.two ? 1 : warps / K;
+        const int room = d.share * 32 * (d.two ? kBeamItems / 2 : kBeamItems);
+        d.merged = (chunks + room - 1) / room;
+        d.pieces = (chunks + d.merged - 1) / d.merged;
+        d.used = (d.pieces + d.share * 32 - 1) / (d.share * 32);
+        return d;
+    }
+    // Warps: as few of 8, 16 and 32 as hold every chunk as a piece of its own, otherwise 32.
+    __host__ __device__ static int warps(int K, int chunks) {
+        for (int w = 8; w < 32; w *= 2)
+            if (K <= w && make(K, chunks, w).merged == 1) return w;
+        return 32;
+    }
+};
 
 struct BeamParams {
     const void* z;               // [B * K, V] logits, rows ld elements apart
@@ -36,10 +59,7 @@ struct BeamParams {
     const uint8_t* finished;     // [B, K] or null
     float2* stats;               // [B * K][chunks]
     int chunks;
-    double* cand_score;          // [B * K][n] the best of each row, best first, and how many
-    int32_t* cand_token;
-    int32_t* cand_count;         // [B * K]
-    unsigned int* tickets;       // [B], zero between calls
+    BeamDeal deal;
     float* score_out;            // [B, n]
     int32_t* parent;
     int32_t* token;
@@ -106,253 +126,335 @@ __global__ void __launch_bounds__(kBeamStatWarps * 32) beam_stats_kernel(const B
 // ---------------------------------------------------------------------------------------------
 // the selection
 // ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned long long ordered_bits64(double x) {
+    const unsigned long long u = static_cast<unsigned long long>(__double_as_longlong(__dadd_rn(x, 0.0)));   // (-0 is 0)
+    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
+}
+__device__ __forceinline__ double from_ordered_bits64(unsigned long long k) {
+    return __longlong_as_double(static_cast<long long>((k >> 63) ? (k & 0x7fffffffffffffffull) : ~k));
+}
+
 // Sum over the block; s is two sets of words, used in turn (one barrier).
-__device__ __forceinline__ int block_sum(int x, int (*s)[kBeamThreads / 32], int& turn) {
+template <int WARPS>
+__device__ __forceinline__ int block_sum(int x, int (*s)[32], int& turn) {
     x = __reduce_add_sync(kFullMask, x);
     if ((threadIdx.x & 31) == 0) s[turn][threadIdx.x >> 5] = x;
     __syncthreads();
-    int sum = 0;
-#pragma unroll
-    for (int i = 0; i < kBeamThreads / 32; ++i) sum += s[turn][i];
+    const int lane = threadIdx.x & 31;
+    x = __reduce_add_sync(kFullMask, lane < WARPS ? s[turn][lane] : 0);
     turn ^= 1;
-    return sum;
+    return x;
 }
 
-// A threshold that between `want` and `cap` (>= want >= 1) of the N keys reach, or all of them where there are no more than cap: key(i)
-// is 0 for what does not take part, and no two others are equal.  Bisection between lo, which more than cap reach, and hi, which fewer than
-// want do, so that it ends when hi = lo + 1 at the latest.  *count: how many reach it.
-template <typename Key>
-__device__ __forceinline__ unsigned long long block_threshold(Key key, int N, int want, int cap, unsigned long long largest,
-                                                              int (*s)[kBeamThreads / 32], int& turn, int* count) {
-    auto reach = [&](unsigned long long t) {
-        int c = 0;
-        for (int i = threadIdx.x; i < N; i += kBeamThreads) c += key(i) >= t;
-        return block_sum(c, s, turn);
-    };
-    unsigned long long lo = 1ull, hi = largest + 1ull;
-    int c = reach(lo);
-    unsigned long long t = lo;
-    while (c > cap && hi - lo > 1ull) {
+// A cut (t, limit) through candidates that are ordered by key, largest first, and then by place: at least `want` and at most `cap` (>= want)
+// of them have key > t, or key == t and place <= limit.  reach(t, limit) counts those, over the block.  Starts from lo, which at least
+// `want` reach (or all, where there are fewer), and hi, which none does; two bisections, the second one where many are equal.
+template <typename Reach>
+__device__ __forceinline__ void block_cut(Reach reach, unsigned long long lo, unsigned long long hi, long long last_place, int want, int cap,
+                                          unsigned long long& t, long long& limit) {
+    t = lo;
+    limit = last_place;
+    if (reach(t, limit) <= cap) return;
+#pragma unroll 1
+    while (hi - lo > 1ull) {
         t = lo + (hi - lo) / 2;
-        c = reach(t);
-        if (c < want) {
-            hi = t;
-            c = cap + 1;
-        } else if (c > cap) {
-            lo = t;
-        }
+        const int c = reach(t, limit);
+        if (c < want) hi = t;
+        else if (c <= cap) return;
+        else lo = t;
     }
-    *count = c;
-    return t;
+    t = lo;    // reached by too many, and what is above it by too few
+    long long below = -1;
+#pragma unroll 1
+    while (limit - below > 1) {
+        const long long mid = below + (limit - below) / 2;
+        if (reach(t, mid) >= want) limit = mid;
+        else below = mid;
+    }
 }
 
-__device__ __forceinline__ unsigned long long ordered_bits64(double x) {
-    const unsigned long long u = static_cast<unsigned long long>(__double_as_longlong(x));
-    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
-}
-
-// A CTA to a row; the last one of a sequence to be done goes on to its beams' candidates.
-template <typename T, int CHUNK>
-__global__ void __launch_bounds__(kBeamThreads) beam_select_kernel(const BeamParams p) {
-    extern __shared__ uint32_t s_keys[];      // [min(chunks, kBeamSmemKeys)]
-    __shared__ unsigned long long s_list[kBeamList];
-    __shared__ int32_t s_pos[kBeamList];      // chunks of the row; then places of the candidates
-    __shared__ int s_sum[2][kBeamThreads / 32];
-    __shared__ double s_dsum[kBeamThreads / 32];
-    __shared__ float s_max[kBeamThreads / 32];
-    __shared__ int s_count, s_last;
-    __shared__ int s_counts[kBeamMaxBeams];
-    static_assert(kBeamChunkList <= kBeamList, "");
-
+// A CTA to a sequence.
+//   1  each row's soft-max statistics from its chunks'
+//   2  the pieces that may hold the n best: every piece is known by its best score.  The n-th largest of what the threads have at best is
+//      reached by n pieces at least, and by few more
+//   3  the logits of these pieces, of which those count that reach the same score
+//   4  what is left is scored in 64 bits and ranked by counting
+// Up to 4 everything is in fp32 with a bound on its error, from which a piece or a logit is dropped only if it cannot be among the n best:
+// the 64-bit units are too few for a score for every piece (of 32000 logits and 4 beams, 8400 and 4400 cycles for steps 1 and 2 in 64 bits).
+// Where too many are equal for the lists (a call that is full of ties), the cuts are made in 64 bits, by bisection.
+template <typename T, int CHUNK, int THREADS>
+__global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p) {
+    constexpr int kWarps = THREADS / 32;
+    __shared__ unsigned long long s_key[kBeamList];
+    __shared__ long long s_place[kBeamList];
+    __shared__ int2 s_piece[kBeamPieceList];
+    __shared__ int s_sum[2][32];
+    __shared__ float s_max[2][32];
+    __shared__ double s_exp[2][32];
+    __shared__ double s_lse[kBeamMaxBeams];     // the sum of exponentials, then what is taken off a logit
+    __shared__ float s_score[kBeamMaxBeams], s_top[kBeamMaxBeams], s_offset[kBeamMaxBeams], s_err[kBeamMaxBeams];
+    __shared__ int s_state[kBeamMaxBeams];      // 0: no continuation, 1: expands, 2: finished
+    __shared__ int s_pieces, s_count;
+    __shared__ uint32_t s_best;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int row = blockIdx.x, b = row / p.K;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int turn = 0;
-    const float c = p.score[row];
-    const bool over = p.finished && p.finished[row];
-    double* cand_score = p.cand_score + (long long)row * p.n;
-    int32_t* cand_token = p.cand_token + (long long)row * p.n;
-    int found = 0;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const BeamDeal deal = p.deal;
+    const int warp_row = deal.two ? warp : warp / deal.share, warp_share = deal.two ? 0 : warp - warp_row * deal.share;
+    constexpr int kHalf = kBeamItems / 2;
+    auto item_row = [&](int j) { return deal.two && j >= kHalf ? warp_row + 32 : warp_row; };
+    auto item_piece = [&](int j) { return ((deal.two ? j & (kHalf - 1) : j) * deal.share + warp_share) * 32 + lane; };
+    auto item_used = [&](int j) { return (deal.two ? j & (kHalf - 1) : j) < deal.used; };
+    auto piece_place = [&](int j) { return item_row(j) * deal.pieces + item_piece(j); };
 
-    if (beam_lives(c) && over) {
-        if (tid == 0) cand_score[0] = c, cand_token[0] = p.eos;
-        found = 1;
-    } else if (beam_lives(c)) {
-        // soft-max statistics of the row
-        const float2* stats = p.stats + (long long)row * p.chunks;
-        const bool held = p.chunks <= kBeamSmemKeys;
-        float m = DISCO_NEG_INF;
-        for (int i = tid; i < p.chunks; i += kBeamThreads) {
-            const float x = __ldcg(&stats[i].x);
-            m = max_nan(m, x);
-            if (held) s_keys[i] = x > DISCO_NEG_INF ? ordered_bits(__fadd_rn(x, 0.f)) : 0u;
-        }
-        m = warp_max_nan_f32(m);
-        if (lane == 0) s_max[warp] = m;
-        if (tid == 0) s_count = 0;
-        __syncthreads();
-        m = s_max[0];
+    // ---- 1 ----
+    float best[kBeamItems];
+    {
+        float m[2] = {DISCO_NEG_INF, DISCO_NEG_INF}, e[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 1; i < kBeamThreads / 32; ++i) m = max_nan(m, s_max[i]);
-        if (m > DISCO_NEG_INF && m < -DISCO_NEG_INF) {   // (otherwise the row is no distribution)
-            double sum = 0.0;
-            for (int i = tid; i < p.chunks; i += kBeamThreads) {
-                const float2 x = __ldcg(&stats[i]);
-                if (x.x > DISCO_NEG_INF) sum += static_cast<double>(x.y) * static_cast<double>(expf(x.x - m));
+        for (int j = 0; j < kBeamItems; ++j) best[j] = DISCO_NEG_INF;
+#pragma unroll 1
+        for (int g = 0; g < deal.merged; ++g) {
+            float2 x[kBeamItems];
+            float top[2] = {DISCO_NEG_INF, DISCO_NEG_INF};
+#pragma unroll
+            for (int j = 0; j < kBeamItems; ++j) {
+                x[j] = make_float2(DISCO_NEG_INF, 0.f);
+                if (item_used(j)) {
+                    const int k = item_row(j), piece = item_piece(j), chunk = piece * deal.merged + g;
+                    if (k < p.K && chunk < p.chunks && piece < deal.pieces) x[j] = __ldcg(p.stats + (long long)(b * p.K + k) * p.chunks + chunk);
+                }
             }
+            if (g == 0) {
+                if (tid < p.K) {
+                    const float c = p.score[b * p.K + tid];
+                    const bool over = p.finished && p.finished[b * p.K + tid];
+                    s_score[tid] = c;
+                    s_state[tid] = !beam_lives(c) ? 0 : over ? 2 : 1;
+                }
+                if (tid == 0) s_count = 0, s_pieces = 0, s_best = 0u;
+            }
+#pragma unroll
+            for (int j = 0; j < kBeamItems; ++j) {
+                if (!item_used(j)) continue;
+                const bool r = deal.two && j >= kHalf;
+                best[j] = max_nan(best[j], x[j].x);
+                top[0] = max_nan(top[0], r ? DISCO_NEG_INF : x[j].x);
+                top[1] = max_nan(top[1], r ? x[j].x : DISCO_NEG_INF);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                if (r == 1 && !deal.two) continue;
+                const float now = max_nan(m[r], warp_max_nan_f32(top[r]));
+                if (now > m[r]) e[r] *= m[r] > DISCO_NEG_INF ? __expf(m[r] - now) : 0.f;
+                m[r] = now;
+#pragma unroll
+                for (int j = 0; j < kBeamItems; ++j)
+                    if (item_used(j) && (deal.two && j >= kHalf) == (r == 1) && x[j].x > DISCO_NEG_INF) e[r] = fmaf(x[j].y, __expf(x[j].x - now), e[r]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            if (r == 1 && !deal.two) continue;
+            double sum = e[r];
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(kFullMask, sum, off);
-            if (lane == 0) s_dsum[warp] = sum;
-            // the chunks that hold the n best
-            auto chunk_key = [&](int i) -> unsigned long long {
-                uint32_t k;
-                if (held) {
-                    k = s_keys[i];
-                } else {
-                    const float x = __ldcg(&stats[i].x);
-                    k = x > DISCO_NEG_INF ? ordered_bits(__fadd_rn(x, 0.f)) : 0u;
-                }
-                return k ? (static_cast<unsigned long long>(k) << 32) | (0xffffffffu - static_cast<uint32_t>(i)) : 0ull;
-            };
-            const unsigned long long largest = (static_cast<unsigned long long>(ordered_bits(__fadd_rn(m, 0.f))) << 32) | 0xffffffffull;
-            int L = 0;
-            const unsigned long long t = block_threshold(chunk_key, p.chunks, p.n, 2 * p.n + 6, largest, s_sum, turn, &L);
-            for (int i = tid; i < p.chunks; i += kBeamThreads)
-                if (chunk_key(i) >= t) s_pos[atomicAdd(&s_count, 1)] = i;
-            // their logits; where there are n chunks, none below the least of their largest counts
-            const uint32_t floor_key = L >= p.n ? static_cast<uint32_t>(t >> 32) : 1u;
-            const T* z = static_cast<const T*>(p.z) + (long long)row * p.ld;
-            __syncthreads();
-            auto value_key = [&](int i) -> unsigned long long {
-                const int v = s_pos[i / CHUNK] * CHUNK + i % CHUNK;
-                if (v >= p.V) return 0ull;
-                const float x = load_logit(z + v);
-                const uint32_t k = x > DISCO_NEG_INF ? ordered_bits(__fadd_rn(x, 0.f)) : 0u;
-                return k >= floor_key ? (static_cast<unsigned long long>(k) << 32) | (0xffffffffu - static_cast<uint32_t>(v)) : 0ull;
-            };
-            if (tid == 0) s_count = 0;
-            __syncthreads();
-            for (int i = tid; i < L * CHUNK; i += kBeamThreads) {
-                const unsigned long long k = value_key(i);
-                if (k) {
-                    const int at = atomicAdd(&s_count, 1);
-                    if (at < kBeamList) s_list[at] = k;
-                }
-            }
-            __syncthreads();
-            int N = s_count;
-            if (N > kBeamList) {   // many equal logits
-                const unsigned long long u = block_threshold(value_key, L * CHUNK, p.n, kBeamList, largest, s_sum, turn, &N);
-                if (tid == 0) s_count = 0;
-                __syncthreads();
-                for (int i = tid; i < L * CHUNK; i += kBeamThreads) {
-                    const unsigned long long k = value_key(i);
-                    if (k >= u) s_list[atomicAdd(&s_count, 1)] = k;
-                }
-                __syncthreads();
-            }
-            sum = s_dsum[0];
+            if (lane == 0) s_max[r][warp] = m[r], s_exp[r][warp] = sum;
+        }
+    }
+    __syncthreads();
+    for (int k = warp; k < p.K; k += kWarps) {       // a warp to a row, a lane to a share
+        const int r = k >> 5, w = deal.two ? k & 31 : k * deal.share + lane;
+        const float x = lane < deal.share ? s_max[r][w] : DISCO_NEG_INF;
+        const float top = warp_max_nan_f32(x);
+        const bool is = top > DISCO_NEG_INF && top < -DISCO_NEG_INF;     // (otherwise the row is no distribution)
+        double sum = is && lane < deal.share && x > DISCO_NEG_INF ? s_exp[r][w] * static_cast<double>(__expf(x - top)) : 0.0;
 #pragma unroll
-            for (int i = 1; i < kBeamThreads / 32; ++i) sum += s_dsum[i];
-            for (int i = tid; i < N; i += kBeamThreads) {
-                const unsigned long long k = s_list[i];
-                int rank = 0;
-                for (int j = 0; j < N; ++j) rank += s_list[j] > k;
-                if (rank < p.n) {
-                    const double x = from_ordered_bits(static_cast<uint32_t>(k >> 32));
-                    cand_score[rank] = static_cast<double>(c) + (x - (static_cast<double>(m) + log(sum)));
-                    cand_token[rank] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(k));
-                }
-            }
-            found = min(N, p.n);
+        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(kFullMask, sum, off);
+        if (lane == 0) {
+            if (!is && s_state[k] == 1) s_state[k] = 0;
+            s_lse[k] = sum;
+            s_top[k] = top;
+            // score = logit + offset, and what fp32 makes of that: a few roundings of numbers of these sizes, and those of the logarithm
+            const float ln = logf(static_cast<float>(sum));
+            s_offset[k] = s_score[k] - (top + ln);
+            s_err[k] = (0x1p-21f * fabsf(s_score[k]) + 0x1p-21f * fabsf(top)) + 0x1p-21f * ln;
         }
     }
-    if (tid == 0) p.cand_count[row] = found;
-    __threadfence();
     __syncthreads();
-    if (tid == 0) s_last = atomicAdd(p.tickets + b, 1u) == static_cast<unsigned int>(p.K) - 1u;
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
 
-    // ---- the sequence: candidates of its beams, by score and then by place (beam by beam, each beam's best first) ----
-    if (tid < p.K) s_counts[tid] = __ldcg(p.cand_count + b * p.K + tid);
-    if (tid == 0) s_count = 0, p.tickets[b] = 0u;
-    __syncthreads();
-    const double* scores = p.cand_score + (long long)b * p.K * p.n;
-    const int M = p.K * p.n;
-    auto score_key = [&](int i) -> unsigned long long {
-        return i % p.n < s_counts[i / p.n] ? ordered_bits64(__dadd_rn(__ldcg(scores + i), 0.0)) : 0ull;
-    };
-    unsigned long long t = 1ull;
-    int last = M;            // of those that are equal to t: places up to this one
-    if (M > kBeamList) {
-        int reached = 0;
-        t = block_threshold(score_key, M, p.n, kBeamList, 0xfffffffffffffffeull, s_sum, turn, &reached);
-        if (reached > kBeamList) {
-            // (equal scores: the bisection ended with two neighbours, of which the lower one is reached by too many; it is the one
-            // that a step above is reached by fewer than n)
-            auto above = [&](unsigned long long u) {
-                int x = 0;
-                for (int i = tid; i < M; i += kBeamThreads) x += score_key(i) >= u;
-                return block_sum(x, s_sum, turn);
-            };
-            if (above(t) < p.n) t -= 1ull;
-            const int need = p.n - above(t + 1ull);
-            int lo = -1, hi = M - 1;     // up to place hi there are enough
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                int x = 0;
-                for (int i = tid; i <= mid; i += kBeamThreads) x += score_key(i) == t;
-                if (block_sum(x, s_sum, turn) >= need) hi = mid;
-                else lo = mid;
+    // ---- 2 ----
+    // (a warp's rows, the second one where it has two)
+    float offset[2], err[2];
+    bool expands[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int k = warp_row + 32 * r;
+        expands[r] = (r == 0 || deal.two) && k < p.K && s_state[k] == 1;
+        offset[r] = expands[r] ? s_offset[k] : 0.f;
+        err[r] = expands[r] ? s_err[k] : 0.f;
+    }
+    float low = DISCO_NEG_INF, high[kBeamItems];      // the least that the best of this thread's pieces may score, the most that each may
+#pragma unroll
+    for (int j = 0; j < kBeamItems; ++j) {
+        if (!item_used(j)) continue;
+        const int r = deal.two && j >= kHalf;
+        if (!expands[r]) best[j] = DISCO_NEG_INF;
+        const float f = best[j] + offset[r], e = err[r] + 0x1p-21f * fabsf(best[j]);
+        if (best[j] > DISCO_NEG_INF && f < -DISCO_NEG_INF) low = fmaxf(low, f - e);       // (beyond what fp32 holds: no bound)
+        high[j] = f + e;
+    }
+    // The n-th largest of these bounds, or a little less.  Each step costs a barrier that counts, so the search goes out from the largest
+    // one, in strides that grow until n reach it, and only then halves what is left.
+    {
+        const uint32_t key = ordered_bits(low), top = __reduce_max_sync(kFullMask, key);
+        if (lane == 0) atomicMax(&s_best, top);
+        __syncthreads();
+        uint32_t lo = 0u, hi = s_best + 1u, stride = 1u << 18;       // reached by n, and by fewer
+        bool out = true;
+#pragma unroll 1
+        while (hi - lo > 1u) {
+            const uint32_t at = out ? (s_best > stride ? s_best - stride : 0u) : lo + (hi - lo) / 2;
+            const int c = __syncthreads_count(key >= at);
+            if (c < p.n) {
+                hi = at;
+                stride <<= 2;
+                out = out && stride != 0u && at > 0u;
+            } else {
+                lo = at;
+                out = false;
+                if (c <= 2 * p.n) break;
             }
-            last = hi;
         }
+        low = lo > 0x007fffffu ? from_ordered_bits(lo) : DISCO_NEG_INF;
     }
-    for (int i = tid; i < M; i += kBeamThreads) {
-        const unsigned long long k = score_key(i);
-        if (k > t || (k == t && i <= last)) {
-            const int at = atomicAdd(&s_count, 1);
-            s_list[at] = k;
-            s_pos[at] = i;
+    float floor = low;
+    const int width = deal.merged * CHUNK;
+    auto note_piece = [&](int j) {      // its row and its first token
+        const int at = atomicAdd(&s_pieces, 1);
+        if (at < kBeamPieceList) s_piece[at] = make_int2(item_row(j), item_piece(j) * width);
+    };
+    auto within = [&](int k, float z) { return z > DISCO_NEG_INF && !((z + s_offset[k]) + (s_err[k] + 0x1p-21f * fabsf(z)) < floor); };
+#pragma unroll
+    for (int j = 0; j < kBeamItems; ++j)
+        if (item_used(j) && best[j] > DISCO_NEG_INF && !(high[j] < floor)) note_piece(j);
+    __syncthreads();
+    auto score_of = [&](int k, float z) { return ordered_bits64(static_cast<double>(s_score[k]) + (static_cast<double>(z) - s_lse[k])); };
+    auto finish_lse = [&] {
+        for (int k = tid; k < p.K; k += THREADS) s_lse[k] = static_cast<double>(s_top[k]) + log(s_lse[k]);
+    };
+    int L = s_pieces, turn = 0;
+    const bool crowded = L > kBeamPieceList;
+    if (crowded) {
+        finish_lse();
+        __syncthreads();
+        unsigned long long key[kBeamItems];
+#pragma unroll
+        for (int j = 0; j < kBeamItems; ++j) key[j] = best[j] > DISCO_NEG_INF ? score_of(item_row(j), best[j]) : 0ull;
+        auto pieces_reach = [&](unsigned long long u, long long limit) {
+            int c = 0;
+#pragma unroll
+            for (int j = 0; j < kBeamItems; ++j) c += key[j] > u || (key[j] == u && piece_place(j) <= limit);
+            return block_sum<kWarps>(c, s_sum, turn);
+        };
+        unsigned long long t;
+        long long limit;
+        block_cut(pieces_reach, 1ull, ~0ull, (long long)p.K * deal.pieces, p.n, 2 * p.n, t, limit);
+        if (tid == 0) s_pieces = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kBeamItems; ++j)
+            if (key[j] > t || (key[j] == t && piece_place(j) <= limit)) note_piece(j);
+        // (more pieces than the list holds, so n at least have been found)
+        floor = __double2float_rd(from_ordered_bits64(t));
+        __syncthreads();
+        L = s_pieces;
+    }
+
+    // ---- 3 ----
+    const int values = L * width;
+    auto locate = [&](int i, int& k, int& v) {      // value i of the pieces
+        const int l = deal.merged == 1 ? i / CHUNK : i / width;
+        const int2 piece = s_piece[l];
+        k = piece.x;
+        v = piece.y + (i - l * width);
+        return v < p.V;
+    };
+    auto logit = [&](int k, int v) { return load_logit(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld + v); };
+    auto place_of = [&](int k, int v) { return (long long)k << 32 | v; };
+    auto take = [&](unsigned long long x, long long place) {
+        const int at = atomicAdd(&s_count, 1);
+        if (at < kBeamList) s_key[at] = x, s_place[at] = place;
+    };
+    constexpr int kAhead = 4;
+    bool first = !crowded;
+    for (int i0 = tid; i0 - tid < values; i0 += kAhead * THREADS) {
+        float z[kAhead];
+        int k[kAhead], v[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int i = i0 + a * THREADS;
+            z[a] = i < values && locate(i, k[a], v[a]) ? logit(k[a], v[a]) : DISCO_NEG_INF;
         }
+        if (first) finish_lse();       // (while the loads are on their way)
+        first = false;
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)       // (a logit stands in for its score, which step 4 needs)
+            if (z[a] > DISCO_NEG_INF && within(k[a], z[a])) take(__float_as_uint(z[a]), place_of(k[a], v[a]));
+    }
+    if (first) finish_lse();
+    if (tid < p.K && s_state[tid] == 2) take(0ull, place_of(tid, p.eos));
+    __syncthreads();
+    if (s_count <= kBeamList) {
+        for (int i = tid; i < s_count; i += THREADS) {
+            const int k = static_cast<int>(s_place[i] >> 32);
+            s_key[i] = s_state[k] == 2 ? ordered_bits64(s_score[k]) : score_of(k, __uint_as_float(static_cast<uint32_t>(s_key[i])));
+        }
+    } else {      // many equal logits
+        auto each = [&](auto f) {
+            for (int i = tid; i < values; i += THREADS) {
+                int k, v;
+                if (!locate(i, k, v)) continue;
+                const float z = logit(k, v);
+                if (z > DISCO_NEG_INF && within(k, z)) f(score_of(k, z), place_of(k, v));
+            }
+            if (tid < p.K && s_state[tid] == 2) f(ordered_bits64(s_score[tid]), place_of(tid, p.eos));
+        };
+        auto values_reach = [&](unsigned long long u, long long limit) {
+            int c = 0;
+            each([&](unsigned long long x, long long place) { c += x > u || (x == u && place <= limit); });
+            return block_sum<kWarps>(c, s_sum, turn);
+        };
+        unsigned long long t;
+        long long limit;
+        block_cut(values_reach, 1ull, ~0ull, (long long)kBeamMaxBeams << 32, p.n, kBeamList, t, limit);
+        __syncthreads();
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+        each([&](unsigned long long x, long long place) {
+            if (x > t || (x == t && place <= limit)) take(x, place);
+        });
     }
     __syncthreads();
+
+    // ---- 4 ----
     const int N = s_count;
     const long long out = (long long)b * p.n;
-    // (what is read of the beams is read before anything is written: the outputs may take the inputs' place)
-    constexpr int kEach = kBeamList / kBeamThreads;
-    int rank[kEach], parent[kEach], token[kEach];
-    float score[kEach];
-    bool ends[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        const int i = e * kBeamThreads + tid;
-        rank[e] = p.n;
-        if (i >= N) continue;
-        const unsigned long long key = s_list[i];
-        const int pos = s_pos[i];
-        int r = 0;
-        for (int j = 0; j < N; ++j) r += s_list[j] > key || (s_list[j] == key && s_pos[j] < pos);
-        if (r >= p.n) continue;
-        rank[e] = r;
-        parent[e] = pos / p.n;
-        token[e] = __ldcg(p.cand_token + (long long)b * M + pos);
-        score[e] = static_cast<float>(__ldcg(scores + pos));
-        ends[e] = token[e] == p.eos || (p.finished && p.finished[b * p.K + parent[e]]);
+    for (int i = tid; i < N; i += THREADS) {
+        const unsigned long long x = s_key[i];
+        const long long place = s_place[i];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < N; ++j) rank += s_key[j] > x || (s_key[j] == x && s_place[j] < place);
+        if (rank < p.n) {       // (what is read of the beams has been read: the outputs may take the inputs' place)
+            const int parent = static_cast<int>(place >> 32), token = static_cast<int>(place & 0xffffffffll);
+            p.score_out[out + rank] = static_cast<float>(from_ordered_bits64(x));
+            p.parent[out + rank] = parent;
+            p.token[out + rank] = token;
+            if (p.finished_out) p.finished_out[out + rank] = token == p.eos || s_state[parent] == 2;
+        }
     }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        if (rank[e] >= p.n) continue;
-        p.score_out[out + rank[e]] = score[e];
-        p.parent[out + rank[e]] = parent[e];
-        p.token[out + rank[e]] = token[e];
-        if (p.finished_out) p.finished_out[out + rank[e]] = ends[e];
-    }
-    for (int i = N + tid; i < p.n; i += kBeamThreads) {
+    for (int i = N + tid; i < p.n; i += THREADS) {
         p.score_out[out + i] = DISCO_NEG_INF;
         p.parent[out + i] = -1;
         p.token[out + i] = -1;

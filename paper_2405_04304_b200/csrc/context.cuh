@@ -44,10 +44,6 @@ struct disco_ctx {
     float* int8_scale;             //   and their scales
     int int8_pitch;
     float2* beam_stats;            // [part_rows][ceil(V / kI8Chunk)] soft-max statistics of chunks of logits
-    double* beam_score;            // [part_rows][DISCO_MAX_KEPT] the best candidates of each beam
-    int32_t* beam_token;
-    int32_t* beam_count;           // [part_rows]
-    unsigned int* beam_tickets;    // [part_rows], zero between calls
     int part_slots;                // partials per row the buffers can hold
     void* encode_tiled;            // cuTensorMapEncodeTiled, resolved through the runtime
     void* pointer_attributes;      // cuPointerGetAttributes, the same way

@@ -546,7 +546,6 @@ int disco_create(disco_ctx** out, int V, int d_draft, int d_target, int max_batc
     // R rows take R * (sm_count / ceil(R / 128)) <= 128 * sm_count records
     device(&c->stamped_rec, (size_t)128 * c->sm_count * 80);       // no stamp yet
     device(&c->row_bound, (size_t)2 * c->part_rows * kDbBoundStride * 4);
-    device(&c->beam_tickets, (size_t)c->part_rows * sizeof(unsigned int));
     zero_bytes = dev_bytes;
     device(&c->part_rec, slots * 64);
     device(&c->final_stats, (size_t)c->part_rows * 2 * sizeof(float));
@@ -565,9 +564,6 @@ int disco_create(disco_ctx** out, int V, int d_draft, int d_target, int max_batc
     device(&c->int8_rows, (size_t)c->part_rows * c->int8_pitch);
     device(&c->int8_scale, ((size_t)c->part_rows + 64) * sizeof(float));   // (read in fours)
     device(&c->beam_stats, (size_t)c->part_rows * ((V + (size_t)kI8Chunk - 1) / kI8Chunk) * sizeof(float2));
-    device(&c->beam_score, (size_t)c->part_rows * DISCO_MAX_KEPT * sizeof(double));
-    device(&c->beam_token, (size_t)c->part_rows * DISCO_MAX_KEPT * sizeof(int32_t));
-    device(&c->beam_count, (size_t)c->part_rows * sizeof(int32_t));
     auto pinned = [&](size_t bytes) {
         const size_t at = host_bytes;
         host_bytes += (bytes + 255) & ~(size_t)255;

@@ -141,10 +141,6 @@ BeamParams beam_params(const disco_ctx* c, const void* z, long long ld, int chun
     p.finished = finished;
     p.stats = c->beam_stats;
     p.chunks = (c->V + chunk - 1) / chunk;
-    p.cand_score = c->beam_score;
-    p.cand_token = c->beam_token;
-    p.cand_count = c->beam_count;
-    p.tickets = c->beam_tickets;
     p.score_out = score_out;
     p.parent = parent;
     p.token = token;
@@ -153,9 +149,11 @@ BeamParams beam_params(const disco_ctx* c, const void* z, long long ld, int chun
 }
 
 template <typename T, int CHUNK>
-int launch_beam_select(disco_ctx* c, const BeamParams& p, cudaStream_t st) {
-    const size_t smem = (size_t)std::min(p.chunks, kBeamSmemKeys) * sizeof(uint32_t);
-    const cudaError_t e = launch_after(c, beam_select_kernel<T, CHUNK>, dim3((unsigned)(p.B * p.K)), dim3(kBeamThreads), smem, st, p);
+int launch_beam_select(disco_ctx* c, BeamParams p, cudaStream_t st) {
+    const int warps = BeamDeal::warps(p.K, p.chunks);
+    p.deal = BeamDeal::make(p.K, p.chunks, warps);
+    auto kern = warps == 8 ? beam_select_kernel<T, CHUNK, 256> : warps == 16 ? beam_select_kernel<T, CHUNK, 512> : beam_select_kernel<T, CHUNK, 1024>;
+    const cudaError_t e = launch_after(c, kern, dim3((unsigned)p.B), dim3((unsigned)(32 * warps)), 0, st, p);
     c->launches += 1;
     return cuda_ok(e, "beam_select_kernel launch") ? DISCO_OK : DISCO_ERR_CUDA;
 }

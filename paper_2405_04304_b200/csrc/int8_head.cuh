@@ -234,13 +234,25 @@ __device__ __forceinline__ void store_logit(float* p, float z) { *p = z; }
 __device__ __forceinline__ void store_logit(__nv_bfloat16* p, float z) { *p = __float2bfloat16_rn(z); }
 __device__ __forceinline__ void store_logit(__half* p, float z) { *p = __float2half_rn(z); }
 
-// Soft-max statistics of 32 logits of one hidden row, one per lane: the largest (NaN if there is one that is not a number) and the
-// sum of exp(z - largest).  The sum is taken in units of 2^-26, as integers: one instruction, no order of summation, off by at most
-// 2^-27 a term where the largest term is 1.
-__device__ __forceinline__ float2 warp_chunk_stats(float z) {
-    const float m = warp_max_nan_f32(z);
-    const uint32_t e = m > DISCO_NEG_INF && m < -DISCO_NEG_INF ? __float2uint_rn(__expf(z - m) * 0x1p26f) : 0u;
-    return make_float2(m, static_cast<float>(__reduce_add_sync(kFullMask, e)) * 0x1p-26f);
+// Soft-max statistics of N times 32 logits of one hidden row, one per lane (those of lanes that are not `in` do not count): the largest
+// (NaN if there is one that is not a number) and the sum of exp(z - largest), for lane i < N those of column i, in `mine`.  The sums are
+// taken in units of 2^-26, as integers: one instruction, no order of summation, off by at most 2^-27 a term where the largest term is 1.
+// (The columns go side by side: one after the other, each waits 300 cycles for its two reductions and its exponential.)
+constexpr int kI8StatsBatch = 16;
+template <int N>
+__device__ __forceinline__ void warp_chunk_stats(const float* z, bool in, int lane, float2& mine) {
+    float m[N];
+    uint32_t e[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) m[i] = warp_max_nan_f32(in ? z[i] : DISCO_NEG_INF);
+#pragma unroll
+    for (int i = 0; i < N; ++i)      // (an exponential that is not a number is converted to 0, and so is that of -inf)
+        e[i] = __float2uint_rn(in ? __expf(z[i] - m[i]) * 0x1p26f : 0.f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[i] = __reduce_add_sync(kFullMask, e[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (lane == i) mine = make_float2(m[i], static_cast<float>(e[i]) * 0x1p-26f);
 }
 
 // Vocabulary rows on the TMEM lanes, hidden rows on the columns: a warp's 32 results of a column are neighbours in y, so they go
@@ -384,20 +396,19 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
                     }
                     float acc[32];
                     tmem_ld32(tmem + c, acc);
-                    float2 mine = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        if (c + i < rows) {
-                            const float z = __fmul_rn(__fmul_rn(static_cast<float>(__float_as_int(acc[i])), xs[i]), ws);
-                            if (in) store_logit(y, z);
+                    for (int i = 0; i < 32; ++i) acc[i] = __fmul_rn(__fmul_rn(static_cast<float>(__float_as_int(acc[i])), xs[i]), ws);
+                    if (in) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            if (c + i < rows) store_logit(y, acc[i]);
                             y += p.ldy;
-                            if constexpr (STATS) {
-                                const float2 s = warp_chunk_stats(in ? z : DISCO_NEG_INF);
-                                if (lane == i) mine = s;
-                            }
                         }
                     }
                     if constexpr (STATS) {
+                        float2 mine = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int i = 0; i < 32; i += kI8StatsBatch) warp_chunk_stats<kI8StatsBatch>(acc + i, in, lane - i, mine);
                         if (c + lane < rows) stats[(long long)(c + lane) * p.chunks] = mine;
                     }
                 }
