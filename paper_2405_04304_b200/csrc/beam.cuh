@@ -13,7 +13,7 @@
 #include <cuda_fp16.h>
 
 #include "common.cuh"
-#include "int8_head.cuh"   // warp_chunk_stats
+#include "int8_head.cuh"   // max_nan, warp_max_nan_f32
 
 namespace disco {
 
@@ -73,12 +73,6 @@ __device__ __forceinline__ float load_logit(const __nv_bfloat16* p) {
 __device__ __forceinline__ float load_logit(const __half* p) {
     return __half2float(__ushort_as_half(__ldcg(reinterpret_cast<const unsigned short*>(p))));
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float m;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-    return m;
-}
-
 // Does the row's beam take part, and by its logits?
 __device__ __forceinline__ bool beam_lives(float c) { return c > DISCO_NEG_INF && c < -DISCO_NEG_INF; }
 __device__ __forceinline__ bool beam_expands(const BeamParams& p, int row) {

@@ -112,6 +112,23 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+// Clusters of two CTAs, and programmatic stream serialization where that is on.
+inline int launch_attributes(const disco_ctx* c, bool pair, cudaLaunchAttribute (&attr)[2]) {
+    int n = 0;
+    if (pair) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = 2;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (c->pdl) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    return n;
+}
+
 // Launch a small follow-up kernel with programmatic stream serialization (it waits with griddepcontrol.wait
 // before it reads anything), so that its launch latency hides behind the kernel before it.
 template <typename... KArgs, typename... Args>

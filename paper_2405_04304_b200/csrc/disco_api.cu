@@ -134,23 +134,6 @@ bool encode_bf16_2d(const disco_ctx* c, CUtensorMap* map, const void* base, int 
 }
 
 
-// Clusters of two CTAs, and programmatic stream serialization where that is on.
-int launch_attributes(const disco_ctx* c, bool pair, cudaLaunchAttribute (&attr)[2]) {
-    int n = 0;
-    if (pair) {
-        attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = 2;
-        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
-        ++n;
-    }
-    if (c->pdl) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n].val.programmaticStreamSerializationAllowed = 1;
-        ++n;
-    }
-    return n;
-}
-
 // Vocabulary on the TMEM lanes (umma_tail.cuh): few rows, and the first rows beyond one tile of 128, where the other form
 // multiplies by 256.  In between and beyond it has no fewer multiplications and the dearer epilogue.  (Launches one after
 // the other at the power limit, 32000 x 5120, 34 / 64 / 96 / 130 / 160 / 192 rows: 61.4 -> 56.2, 61.6 -> 58.2, 63.1 -> 62.5,
@@ -562,7 +545,7 @@ int disco_create(disco_ctx** out, int V, int d_draft, int d_target, int max_batc
     device(&c->stage_dev, (2 * (size_t)max_batch + (size_t)max_rows) * sizeof(int32_t));
     c->int8_pitch = (std::max(d_draft, d_target) + 15) & ~15;
     device(&c->int8_rows, (size_t)c->part_rows * c->int8_pitch);
-    device(&c->int8_scale, ((size_t)c->part_rows + 64) * sizeof(float));   // (read in fours)
+    device(&c->int8_scale, (size_t)c->part_rows * sizeof(float));
     device(&c->beam_stats, (size_t)c->part_rows * ((V + (size_t)kI8Chunk - 1) / kI8Chunk) * sizeof(float2));
     auto pinned = [&](size_t bytes) {
         const size_t at = host_bytes;

@@ -82,36 +82,66 @@ int check_head(const disco_ctx* c, const int8_t* W_q, long long ldw, const float
     return d > std::max(c->d_draft, c->d_target) ? DISCO_ERR_WORKSPACE : DISCO_OK;
 }
 
-template <typename Out, bool STATS>
-int launch_int8_head(disco_ctx* c, const int8_t* W_q, long long ldw, const float* w_scale, int d, int R, void* y, long long ldy,
-                     cudaStream_t st) {
+// The product of hidden rows that are in 8 bits already (In = void), or of a few rows of type In.
+template <typename Out, typename In, bool STATS, bool PAIR>
+int launch_int8_head(disco_ctx* c, const int8_t* W_q, long long ldw, const float* w_scale, const void* x, long long ldx, int d, int R, void* y,
+                     long long ldy, cudaStream_t st) {
+    constexpr bool FEW = !std::is_void<In>::value;
     Int8Params p{};
     p.V = c->V;
     p.d = d;
     p.R = R;
-    p.t = Int8Tiling::make(R, c->V, c->sm_count, STATS);
-    p.x_box = std::min(p.t.N, round_up(R, 8));
+    p.t = Int8Tiling::make(R, c->V, c->sm_count, STATS, PAIR);
     p.w_scale = w_scale;
     p.x_scale = c->int8_scale;
+    p.x = x;
+    p.ldx = ldx;
     p.y = y;
     p.ldy = ldy;
     p.stats = STATS ? c->beam_stats : nullptr;
     p.chunks = (c->V + kI8Chunk - 1) / kI8Chunk;
     p.status = c->status;
-    auto kern = int8_head_kernel<Out, STATS>;
+    auto kern = int8_head_kernel<Out, In, STATS, PAIR>;
     static KernelSetup setup;
     size_t limit = 0;
     if (!raise_smem_limit(c, setup, kern, 0, &limit)) return DISCO_ERR_CUDA;
-    p.ring = Int8Ring::make(p.t, (long long)limit);
+    constexpr int kTurn = STATS ? kI8TurnBytes : 0;
+    p.ring = Int8Ring::make(p.t, d, (long long)limit - kTurn, FEW);
     if (p.ring.stages == 0) return DISCO_ERR_UNSUPPORTED_SHAPE;
-    CUtensorMap tmap_W, tmap_X;
-    if (!encode_int8_2d(c, &tmap_W, W_q, c->V, d, ldw, p.t.TR) || !encode_int8_2d(c, &tmap_X, c->int8_rows, R, d, c->int8_pitch, p.x_box))
-        return DISCO_ERR_CUDA;
+    CUtensorMap tmap_W, tmap_X{};
+    if (!encode_int8_2d(c, &tmap_W, W_q, c->V, d, ldw, p.t.w_box)) return DISCO_ERR_CUDA;
+    if (!FEW && !encode_int8_2d(c, &tmap_X, c->int8_rows, R, d, c->int8_pitch, p.t.x_box)) return DISCO_ERR_CUDA;
     const int items = p.t.MT * p.t.NV;
-    const cudaError_t e = launch_after(c, kern, dim3((unsigned)std::min(items, c->sm_count)), dim3(kI8Threads),
-                                       (size_t)(kI8FixedSmem + p.ring.bytes), st, tmap_W, tmap_X, p);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(PAIR ? 2 * std::min(items, c->sm_count / 2) : std::min(items, c->sm_count)));
+    cfg.blockDim = dim3(kI8Threads);
+    cfg.dynamicSmemBytes = (size_t)(kI8FixedSmem + p.ring.bytes + p.ring.resident + kTurn);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    cfg.attrs = attr;
+    cfg.numAttrs = launch_attributes(c, PAIR, attr);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tmap_W, tmap_X, p);
     c->launches += 1;
     return cuda_ok(e, "int8_head_kernel launch") ? DISCO_OK : DISCO_ERR_CUDA;
+}
+
+// Logits of R hidden rows (and, STATS, their soft-max statistics by chunks).
+template <typename Out, bool STATS>
+int project(disco_ctx* c, const int8_t* W_q, long long ldw, const float* w_scale, const void* H, int h_type, long long ldh, int d, int R, void* y,
+            long long ldy, cudaStream_t st) {
+    if (Int8Ring::few(R, d)) {
+        switch (h_type) {
+            case DISCO_F32: return launch_int8_head<Out, float, STATS, false>(c, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
+            case DISCO_BF16: return launch_int8_head<Out, __nv_bfloat16, STATS, false>(c, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
+            default: return launch_int8_head<Out, __half, STATS, false>(c, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
+        }
+    }
+    const int rc = quantize(c, H, h_type, ldh, R, d, c->int8_rows, c->int8_pitch, c->int8_scale, st);
+    if (rc) return rc;
+    static const char* e = getenv("I8PAIR");
+    const bool pair = e ? atoi(e) : R > 128;
+    return pair ? launch_int8_head<Out, void, STATS, true>(c, W_q, ldw, w_scale, nullptr, 0, d, R, y, ldy, st)
+                : launch_int8_head<Out, void, STATS, false>(c, W_q, ldw, w_scale, nullptr, 0, d, R, y, ldy, st);
 }
 
 int check_beams(const disco_ctx* c, int B, int K, int n, const float* score, const uint8_t* finished, int eos, const float* score_out,
@@ -223,12 +253,10 @@ int disco_project_int8(disco_ctx* c, const int8_t* W_q, long long ldw, const flo
     if (!on_its_device(c)) return DISCO_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     c->last_stream = st;
-    rc = quantize(c, H, h_type, ldh, R, d, c->int8_rows, c->int8_pitch, c->int8_scale, st);
-    if (rc) return rc;
     switch (y_type) {
-        case DISCO_F32: return launch_int8_head<float, false>(c, W_q, ldw, w_scale, d, R, y, ldy, st);
-        case DISCO_BF16: return launch_int8_head<__nv_bfloat16, false>(c, W_q, ldw, w_scale, d, R, y, ldy, st);
-        default: return launch_int8_head<__half, false>(c, W_q, ldw, w_scale, d, R, y, ldy, st);
+        case DISCO_F32: return project<float, false>(c, W_q, ldw, w_scale, H, h_type, ldh, d, R, y, ldy, st);
+        case DISCO_BF16: return project<__nv_bfloat16, false>(c, W_q, ldw, w_scale, H, h_type, ldh, d, R, y, ldy, st);
+        default: return project<__half, false>(c, W_q, ldw, w_scale, H, h_type, ldh, d, R, y, ldy, st);
     }
 }
 
@@ -262,9 +290,7 @@ int disco_beam_step_int8(disco_ctx* c, const int8_t* W_q, long long ldw, const f
     if (!on_its_device(c)) return DISCO_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     c->last_stream = st;
-    rc = quantize(c, H, h_type, ldh, R, d, c->int8_rows, c->int8_pitch, c->int8_scale, st);
-    if (rc) return rc;
-    rc = launch_int8_head<float, true>(c, W_q, ldw, w_scale, d, R, work, c->V, st);
+    rc = project<float, true>(c, W_q, ldw, w_scale, H, h_type, ldh, d, R, work, c->V, st);
     if (rc) return rc;
     const BeamParams p = beam_params(c, work, c->V, kI8Chunk, B, K, n, score, finished, eos, score_out, parent, token, finished_out);
     return launch_beam_select<float, kI8Chunk>(c, p, st);

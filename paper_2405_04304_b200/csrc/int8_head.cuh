@@ -7,6 +7,9 @@
 // the sum, times s_x, times s_w.
 #pragma once
 
+#include <cstdlib>
+#include <type_traits>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -35,6 +38,30 @@ __device__ __forceinline__ int quantize_one(float x, float top, float inv) {
     if constexpr (sizeof(T) == 2) return __float2int_rn(__fdiv_rn(x * 0.9921875f, top) * 128.f);
     else return __double2int_rn(__ddiv_rn(127.0 * static_cast<double>(x), static_cast<double>(top)));
 }
+
+// The largest |x| of a row by its bits (whose order is that of the numbers; what is not finite comes above all else), and what follows from it.
+struct RowScale {
+    float top, inv, shift, scale;     // inv = 0: a row of zeros, or one that holds a number that is not finite
+    __device__ __forceinline__ explicit RowScale(uint32_t top_bits) {
+        const bool finite = top_bits < 0x7f800000u;
+        top = __uint_as_float(top_bits);
+        scale = finite ? __fdiv_rn(top, 127.f) : __uint_as_float(0x7fc00000u);
+        // numbers near the smallest ones are shifted up, which is exact
+        shift = top < 0x1p-60f ? 0x1p100f : 1.f;
+        top *= shift;
+        inv = finite && top > 0.f ? 127.f / top : 0.f;
+    }
+    // Eight numbers in 8 bits each.
+    template <typename T>
+    __device__ __forceinline__ uint2 round(const float (&f)[8]) const {
+        uint32_t w[2] = {0u, 0u};
+        if (inv > 0.f) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j >> 2] |= (static_cast<uint32_t>(quantize_one<T>(f[j] * shift, top, inv)) & 0xffu) << (8 * (j & 3));
+        }
+        return make_uint2(w[0], w[1]);
+    }
+};
 
 // Eight consecutive numbers of a row.  (Not by the read-only path: the compiler may move such loads ahead of the wait for the kernel
 // that wrote them.)
@@ -89,13 +116,13 @@ template <typename T, int CH>
 __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const QuantParams p) {
     __shared__ uint32_t s_top[kQuantThreads / 32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    // (only now: what comes next may read the head ahead of its own wait, and the head may be what ran before this)
+    // (not before the wait: what comes next may read the head ahead of its own, and the head may be what ran before this)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const long long row = blockIdx.x;
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const int chunks = p.d >> 3;
     QuantChunk<T> c[CH];
-    uint32_t top_bits = 0u;     // the order of |x| is that of its bits, and what is not finite comes above all else
+    uint32_t top_bits = 0u;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int at = i * kQuantThreads + threadIdx.x;
@@ -112,14 +139,8 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const Quan
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kQuantThreads / 32; ++i) top_bits = max(top_bits, s_top[i]);
-    const bool finite = top_bits < 0x7f800000u;
-    float top = __uint_as_float(top_bits);
-    if (threadIdx.x == 0) p.scale[row] = finite ? __fdiv_rn(top, 127.f) : __uint_as_float(0x7fc00000u);
-    // numbers near the smallest ones are shifted up, which is exact
-    const float shift = top < 0x1p-60f ? 0x1p100f : 1.f;
-    top *= shift;
-    const bool some = finite && top > 0.f;
-    const float inv = some ? 127.f / top : 0.f;
+    const RowScale rs(top_bits);
+    if (threadIdx.x == 0) p.scale[row] = rs.scale;
     int8_t* q = p.q + row * p.ldq;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -127,13 +148,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const Quan
         if (at < chunks) {
             float f[8];
             c[i].get(f);
-            uint32_t w[2] = {0u, 0u};
-            if (some) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    w[j >> 2] |= (static_cast<uint32_t>(quantize_one<T>(f[j] * shift, top, inv)) & 0xffu) << (8 * (j & 3));
-            }
-            *reinterpret_cast<uint2*>(q + 8 * at) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2*>(q + 8 * at) = rs.template round<T>(f);
         }
     }
     if ((p.d & 15) && threadIdx.x == 0) *reinterpret_cast<uint2*>(q + p.d) = make_uint2(0u, 0u);
@@ -144,35 +159,48 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const Quan
 // ---------------------------------------------------------------------------------------------
 constexpr int kI8BK = 128;                // k elements per stage (one 128-byte swizzle span)
 constexpr int kI8MaxStages = 24;
-constexpr int kI8EpiWarps = 8;
+constexpr int kI8EpiWarps = 16;
 constexpr int kI8Threads = (2 + kI8EpiWarps) * 32;
-constexpr int kI8FixedSmem = 1024 /*align*/ + 512 /*barriers*/;
+constexpr int kI8FewChunks = 8;           // of eight numbers, that a lane holds of a row which the kernel rounds itself
+constexpr int kI8FixedSmem = 1024 /*align*/ + 512 /*barriers*/ + 2 * 256 * 4 /*scales of two tiles' hidden rows*/;
 
 __host__ __device__ inline int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
 // How V vocabulary rows and R hidden rows are cut: MT tiles of NT hidden rows (the columns of an accumulator; the MMA takes N of
 // them) times NV tiles of TR vocabulary rows (one or two blocks of 128 TMEM lanes).  Item i is hidden tile i % MT of vocabulary tile
 // i / MT; the CTAs take items in turn, so those that share a vocabulary tile run side by side and the head crosses HBM once.
+//
+// Pairs of CTAs (cta_group::2): a tile's vocabulary rows lie half in each CTA (one block), and so do the hidden rows that both multiply by.
 struct Int8Tiling {
     int MT, NT, N, NV, TR, blocks, cols, bufs;
-    __host__ __device__ static Int8Tiling make(int R, int V, int grid, bool whole_chunks) {
+    int w_box, x_box;      // rows of the boxes that a CTA loads
+    __host__ __device__ static Int8Tiling make(int R, int V, int grid, bool whole_chunks, bool pairs) {
         Int8Tiling t;
+        const int ctas = pairs ? 2 : 1;
         t.MT = (R + 255) / 256;
-        t.N = round_up((R + t.MT - 1) / t.MT, 16);
+#ifndef __CUDA_ARCH__
+        if (getenv("I8MT")) t.MT += atoi(getenv("I8MT"));
+#endif
+        t.N = round_up((R + t.MT - 1) / t.MT, 16 * ctas);
         t.NT = t.N;
         t.MT = (R + t.NT - 1) / t.NT;
         // as few rounds of items as tiles of 256 vocabulary rows need, all items alike
+        const int workers = grid / ctas;
         const long long items = (long long)t.MT * ((V + 255) / 256);
-        const long long rounds = (items + grid - 1) / grid;
-        const long long most = rounds * grid / t.MT;
+        const long long rounds = (items + workers - 1) / workers;
+        const long long most = rounds * workers / t.MT;
         const int nv = (int)(most < V ? (most > 1 ? most : 1) : V);
-        t.TR = (V + nv - 1) / nv;
-        if (whole_chunks) t.TR = round_up(t.TR, kI8Chunk);
+        t.TR = round_up((V + nv - 1) / nv, ctas * (whole_chunks ? kI8Chunk : 1));
         if (t.TR > 256) t.TR = 256;
+#ifndef __CUDA_ARCH__
+        if (getenv("I8TR")) t.TR = atoi(getenv("I8TR"));
+#endif
         t.NV = (V + t.TR - 1) / t.TR;
-        t.blocks = t.TR > 128 ? 2 : 1;
+        t.blocks = t.TR > 128 && !pairs ? 2 : 1;
         t.cols = round_up(t.N, 32);
         t.bufs = 2 * t.blocks * t.cols <= 512 ? 2 : 1;
+        t.w_box = t.TR / ctas;
+        t.x_box = pairs ? t.N / 2 : (round_up(R, 8) < t.N ? round_up(R, 8) : t.N);
         return t;
     }
 };
@@ -181,19 +209,28 @@ struct Int8Tiling {
 // a block and all N hidden rows: what lies behind the boxes (always inside the ring) only feeds accumulators that nobody reads.
 struct Int8Ring {
     int stages, w_bytes, x_bytes, bytes;
+    int resident;       // bytes behind the stages: all of the hidden rows (then x_bytes is 0)
     __host__ __device__ static int size(const Int8Ring& r, const Int8Tiling& t, int stages) {
         const int all = stages * (r.w_bytes + r.x_bytes), last = (stages - 1) * r.w_bytes + t.blocks * 128 * kI8BK;
         return round_up(all > last ? all : last, 1024);
     }
-    // As many stages as fit `limit` bytes; none if that is less than two.
-    __host__ __device__ static Int8Ring make(const Int8Tiling& t, long long limit) {
+    // As many stages as fit `limit` bytes beside the fixed part; none if that is less than two.
+    __host__ __device__ static Int8Ring make(const Int8Tiling& t, int d, long long limit, bool few) {
         Int8Ring r{};
-        r.w_bytes = round_up(t.TR * kI8BK, 1024);
-        r.x_bytes = t.N * kI8BK;
+        r.w_bytes = round_up(t.w_box * kI8BK, 1024);
+        r.x_bytes = few ? 0 : round_up(t.x_box, 16) * kI8BK;      // (all that an MMA reads: N rows, or half of them in each CTA)
+        r.resident = few ? (d + kI8BK - 1) / kI8BK * t.N * kI8BK : 0;
         int stages = kI8MaxStages;
-        while (stages >= 2 && kI8FixedSmem + size(r, t, stages) > limit) --stages;
+        while (stages >= 2 && kI8FixedSmem + size(r, t, stages) + r.resident > limit) --stages;
         if (stages >= 2) r.stages = stages, r.bytes = size(r, t, stages);
         return r;
+    }
+    // Hidden rows that the kernel rounds itself, in every CTA (its epilogue's warps have nothing else to do meanwhile): where they are few
+    // enough for a lane to hold its part of them, and to lie in shared memory beside the stages.  (A pass of 1 row of a 32000 x 768 head
+    // 9.6 -> 7.4 us; with rows that are read twice, 11 of 32000 x 5120 30 -> 42.)
+    __host__ __device__ static bool few(int R, int d) {
+        if (R > kI8EpiWarps || (d + kI8BK - 1) / kI8BK * 16 * kI8BK > 96 * 1024) return false;
+        return d <= kI8EpiWarps / R * 256 * kI8FewChunks;
     }
 };
 
@@ -201,9 +238,10 @@ struct Int8Params {
     int V, d, R;
     Int8Tiling t;
     Int8Ring ring;
-    int x_box;                 // rows of the hidden-row box (a multiple of 8, <= N)
     const float* w_scale;      // [V]
-    const float* x_scale;      // [R], 16-byte aligned, with room behind for 32 more
+    const float* x_scale;      // [R]
+    const void* x;             // FEW: the hidden rows themselves, ldx elements apart
+    long long ldx;
     void* y;
     long long ldy;
     float2* stats;             // [R][chunks] (largest logit of the chunk, sum of exp(z - largest)), or null
@@ -216,6 +254,14 @@ __device__ __forceinline__ void tc_mma_i8(uint32_t d_tmem, uint64_t a_desc, uint
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tc_mma_i8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
         "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
@@ -234,25 +280,49 @@ __device__ __forceinline__ void store_logit(float* p, float z) { *p = z; }
 __device__ __forceinline__ void store_logit(__nv_bfloat16* p, float z) { *p = __float2bfloat16_rn(z); }
 __device__ __forceinline__ void store_logit(__half* p, float z) { *p = __float2half_rn(z); }
 
-// Soft-max statistics of N times 32 logits of one hidden row, one per lane (those of lanes that are not `in` do not count): the largest
-// (NaN if there is one that is not a number) and the sum of exp(z - largest), for lane i < N those of column i, in `mine`.  The sums are
-// taken in units of 2^-26, as integers: one instruction, no order of summation, off by at most 2^-27 a term where the largest term is 1.
-// (The columns go side by side: one after the other, each waits 300 cycles for its two reductions and its exponential.)
-constexpr int kI8StatsBatch = 16;
-template <int N>
-__device__ __forceinline__ void warp_chunk_stats(const float* z, bool in, int lane, float2& mine) {
-    float m[N];
-    uint32_t e[N];
+// Soft-max statistics of 32 vocabulary rows' logits, one per lane, of 16 hidden rows: the largest of each hidden row's (NaN if there is
+// one that is not a number) and the sum of exp(z - largest).  By way of a corner turn in shared memory: two lanes to a hidden row, 16
+// logits each.  // turn: 16 x kI8TurnStride floats of the warp.  Lane i and lane i + 16 return those of hidden row i.
+constexpr int kI8TurnStride = 33;
+constexpr int kI8TurnBytes = kI8EpiWarps * 16 * kI8TurnStride * 4;
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+__device__ __forceinline__ float2 warp_chunk_stats(const float* z, bool in, int lane, float* turn) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) m[i] = warp_max_nan_f32(in ? z[i] : DISCO_NEG_INF);
+    for (int i = 0; i < 16; ++i) turn[i * kI8TurnStride + lane] = in ? z[i] : DISCO_NEG_INF;
+    __syncwarp();
+    const float* mine = turn + (lane & 15) * kI8TurnStride + (lane & 16);
+    float x[16];
 #pragma unroll
-    for (int i = 0; i < N; ++i)      // (an exponential that is not a number is converted to 0, and so is that of -inf)
-        e[i] = __float2uint_rn(in ? __expf(z[i] - m[i]) * 0x1p26f : 0.f);
+    for (int j = 0; j < 16; ++j) x[j] = mine[j];
+    __syncwarp();
+    float m = x[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i) e[i] = __reduce_add_sync(kFullMask, e[i]);
+    for (int j = 1; j < 16; ++j) m = max_nan(m, x[j]);
+    m = max_nan(m, __shfl_xor_sync(kFullMask, m, 16));
+    float e[2] = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (lane == i) mine = make_float2(m[i], static_cast<float>(e[i]) * 0x1p-26f);
+    for (int j = 0; j < 16; ++j) e[j & 1] += __expf(x[j] - m);
+    float sum = e[0] + e[1];
+    sum += __shfl_xor_sync(kFullMask, sum, 16);
+    return make_float2(m, sum);      // (NaN where the largest is not finite: nothing is done with it there)
+}
+
+// 32 lanes x 16 consecutive 32-bit columns -> 16 registers per thread
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, int (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
 
 // Vocabulary rows on the TMEM lanes, hidden rows on the columns: a warp's 32 results of a column are neighbours in y, so they go
@@ -260,24 +330,31 @@ __device__ __forceinline__ void warp_chunk_stats(const float* z, bool in, int la
 //   * warp 0    producer: a box of TR vocabulary rows x 128 k and one of the tile's hidden rows per stage
 //   * warp 1    MMA issuer: M = 128 (twice for more than 128 vocabulary rows), N = hidden rows of the tile, K = 32
 //   * warps 2+  epilogue: a thread owns a vocabulary row and walks over the hidden rows
-template <typename Out, bool STATS>
+template <typename Out, typename In, bool STATS, bool PAIR>
 __global__ void __launch_bounds__(kI8Threads, 1)
 int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_constant__ CUtensorMap tmap_X, const Int8Params p) {
+    constexpr bool FEW = !std::is_void<In>::value;
+    static_assert(!(FEW && PAIR), "");
     extern __shared__ uint8_t smem_dyn[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
     uint8_t* w_tiles = smem;
-    uint8_t* x_tiles = smem + p.ring.stages * p.ring.w_bytes;
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + p.ring.bytes);
+    uint8_t* x_tiles = FEW ? smem + p.ring.bytes : smem + p.ring.stages * p.ring.w_bytes;
+    uint8_t* fixed = smem + p.ring.bytes + (FEW ? p.ring.resident : 0);
+    uint64_t* full = reinterpret_cast<uint64_t*>(fixed);
     uint64_t* empty = full + kI8MaxStages;
     uint64_t* tmem_full = empty + kI8MaxStages;
     uint64_t* tmem_empty = tmem_full + 2;
-    uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(tmem_empty + 2);
+    uint64_t* rows_full = tmem_empty + 2;
+    uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(rows_full + 1);
 
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
     const Int8Tiling& t = p.t;
     const int KB = (p.d + kI8BK - 1) / kI8BK;
     const int items = t.MT * t.NV;
+    const int rank = PAIR ? (int)cluster_rank() : 0;
+    const bool leader = rank == 0;
+    const int worker = PAIR ? (int)blockIdx.x >> 1 : (int)blockIdx.x, workers = PAIR ? (int)gridDim.x >> 1 : (int)gridDim.x;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.ring.stages; ++s) {
@@ -286,18 +363,24 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&tmem_full[b], 1);
-            mbar_init(&tmem_empty[b], kI8EpiWarps);
+            mbar_init(&tmem_empty[b], PAIR ? 2 * kI8EpiWarps : kI8EpiWarps);
         }
+        mbar_init(rows_full, kI8EpiWarps);
         fence_mbar_init();
         prefetch_tensormap(&tmap_W);
-        prefetch_tensormap(&tmap_X);
+        if (!FEW) prefetch_tensormap(&tmap_X);
     }
     if (warp == 1) {
-        tmem_alloc(tmem_base_s, 512);
-        tmem_relinquish();
+        if constexpr (PAIR) {
+            tmem_alloc_pair(tmem_base_s, 512);
+        } else {
+            tmem_alloc(tmem_base_s, 512);
+            tmem_relinquish();
+        }
     }
     tc_fence_before();
-    __syncthreads();
+    if constexpr (PAIR) cluster_sync();
+    else __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_base_s;
 
@@ -305,46 +388,72 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
         // ------------------------------ producer ------------------------------
         if (elect_one()) {
             const uint32_t full0 = smem_addr(full), empty0 = smem_addr(empty), w0 = smem_addr(w_tiles), x0 = smem_addr(x_tiles);
-            const uint32_t expected = (uint32_t)(t.TR + p.x_box) * 128u;
-            const int k_end = KB * kI8BK;
-            int item = blockIdx.x;
+            // (a pair's loads are counted on the leader's barriers)
+            const uint32_t count0 = PAIR ? leader_addr(full0) : full0, expected = (PAIR ? 2 : 1) * (uint32_t)(t.w_box + (FEW ? 0 : t.x_box)) * 128u;
+            const int k_end = KB * kI8BK, v_own = rank * t.w_box, r_own = rank * t.x_box;
+            auto load = [&](uint32_t dst, const CUtensorMap* map, int c0, int c1, int slot) {
+                if constexpr (PAIR) tma_load_2d_pair(dst, map, c0, c1, count0 + slot * 8);
+                else tma_load_2d(dst, map, c0, c1, count0 + slot * 8);
+            };
+            int item = worker;
             // The head is complete before the kernel that rounds the hidden rows lets this one start: its first tiles are
             // requested at once, the hidden rows of the same stages behind the wait for that kernel.
+            // (FEW: what ran before this may have written the head.)
+            if (FEW) asm volatile("griddepcontrol.wait;" ::: "memory");
             const int pre = item < items ? min(p.ring.stages, KB) : 0;
             for (int n = 0; n < pre; ++n) {
-                mbar_arrive_expect_tx(full0 + n * 8, expected);
-                tma_load_2d(w0 + n * p.ring.w_bytes, &tmap_W, n * kI8BK, item / t.MT * t.TR, full0 + n * 8);
+                if (leader) mbar_arrive_expect_tx(full0 + n * 8, expected);
+                load(w0 + n * p.ring.w_bytes, &tmap_W, n * kI8BK, item / t.MT * t.TR + v_own, n);
             }
-            asm volatile("griddepcontrol.wait;" ::: "memory");
+            if (!FEW) asm volatile("griddepcontrol.wait;" ::: "memory");
             asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-            for (int n = 0; n < pre; ++n)
-                tma_load_2d(x0 + n * p.ring.x_bytes, &tmap_X, n * kI8BK, item % t.MT * t.NT, full0 + n * 8);
+            for (int n = 0; !FEW && n < pre; ++n) load(x0 + n * p.ring.x_bytes, &tmap_X, n * kI8BK, item % t.MT * t.NT + r_own, n);
             int stage = pre == p.ring.stages ? 0 : pre, phase = pre == p.ring.stages ? 1 : 0;
             int k = pre * kI8BK;
-            for (; item < items; item += gridDim.x, k = 0) {
-                const int v0 = item / t.MT * t.TR, r0 = item % t.MT * t.NT;
+            for (; item < items; item += workers, k = 0) {
+                const int v0 = item / t.MT * t.TR + v_own, r0 = item % t.MT * t.NT + r_own;
                 for (; k < k_end; k += kI8BK) {
-                    const uint32_t bar = full0 + stage * 8;
                     mbar_wait(empty0 + stage * 8, phase ^ 1, p.status);
-                    mbar_arrive_expect_tx(bar, expected);
-                    tma_load_2d(w0 + stage * p.ring.w_bytes, &tmap_W, k, v0, bar);
-                    tma_load_2d(x0 + stage * p.ring.x_bytes, &tmap_X, k, r0, bar);
+                    if (leader) mbar_arrive_expect_tx(full0 + stage * 8, expected);
+                    load(w0 + stage * p.ring.w_bytes, &tmap_W, k, v0, stage);
+                    if (!FEW) load(x0 + stage * p.ring.x_bytes, &tmap_X, k, r0, stage);
+                    if (++stage == p.ring.stages) stage = 0, phase ^= 1;
+                }
+            }
+            if constexpr (PAIR) {   // the leader's arrivals at this CTA's barriers are all in before it leaves
+                for (int n = 0; n < p.ring.stages; ++n) {
+                    mbar_wait(empty0 + stage * 8, phase ^ 1, p.status);
                     if (++stage == p.ring.stages) stage = 0, phase ^= 1;
                 }
             }
         }
     } else if (warp == 1) {
         // ------------------------------ MMA issuer ------------------------------
-        if (elect_one()) {
-            const uint32_t idesc = umma_idesc_i8(t.N);
+        if (leader && elect_one()) {
+            const uint32_t idesc = umma_idesc_i8(t.N, PAIR ? 256 : 128);
+            auto mma = [&](uint32_t d, uint64_t w, uint64_t x, uint32_t accumulate) {
+                if constexpr (PAIR) tc_mma_i8_pair(d, w, x, idesc, accumulate);
+                else tc_mma_i8(d, w, x, idesc, accumulate);
+            };
+            auto commit = [&](uint32_t bar) {
+                if constexpr (PAIR) tc_commit_pair(bar);
+                else tc_commit(bar);
+            };
             const uint32_t full0 = smem_addr(full), empty0 = smem_addr(empty);
             const uint64_t w_desc0 = umma_smem_desc(w_tiles), x_desc0 = umma_smem_desc(x_tiles);
-            const uint32_t w_step = (uint32_t)p.ring.w_bytes >> 4, x_step = (uint32_t)p.ring.x_bytes >> 4;   // descriptor units
+            const uint32_t w_step = (uint32_t)p.ring.w_bytes >> 4, x_step = (FEW ? (uint32_t)t.N * kI8BK : (uint32_t)p.ring.x_bytes) >> 4;   // descriptor units
             uint64_t w_desc = w_desc0, x_desc = x_desc0;
             int stage = 0, phase = 0, it = 0;
-            for (int item = blockIdx.x; item < items; item += gridDim.x, ++it) {
+            if (FEW) {
+                mbar_wait(rows_full, 0, p.status);
+                tc_fence_after();
+            }
+            for (int item = worker; item < items; item += workers, ++it) {
+                if (FEW) x_desc = x_desc0;
                 const int b = t.bufs == 2 ? it & 1 : 0;
-                mbar_wait(&tmem_empty[b], ((t.bufs == 2 ? it >> 1 : it) & 1) ^ 1, p.status);
+                const uint32_t parity = ((t.bufs == 2 ? it >> 1 : it) & 1) ^ 1;
+                if constexpr (PAIR) mbar_wait_cluster(smem_addr(&tmem_empty[b]), parity, p.status);
+                else mbar_wait(&tmem_empty[b], parity, p.status);
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + b * t.blocks * t.cols;
                 for (int kb = 0; kb < KB; ++kb) {
@@ -352,78 +461,142 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
                     tc_fence_after();
 #pragma unroll
                     for (int k = 0; k < 4; ++k)       // 32 k elements = 32 bytes = 2 descriptor units
-                        tc_mma_i8(d_tmem, w_desc + 2 * k, x_desc + 2 * k, idesc, (kb | k) != 0);
-                    if (t.blocks == 2) {
+                        mma(d_tmem, w_desc + 2 * k, x_desc + 2 * k, (kb | k) != 0);
+                    if (!PAIR && t.blocks == 2) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)   // 128 vocabulary rows further on
-                            tc_mma_i8(d_tmem + t.cols, w_desc + (128 * 128 >> 4) + 2 * k, x_desc + 2 * k, idesc, (kb | k) != 0);
+                            mma(d_tmem + t.cols, w_desc + (128 * 128 >> 4) + 2 * k, x_desc + 2 * k, (kb | k) != 0);
                     }
-                    tc_commit(empty0 + stage * 8);
+                    commit(empty0 + stage * 8);
                     w_desc += w_step;
                     x_desc += x_step;
-                    if (++stage == p.ring.stages) stage = 0, phase ^= 1, w_desc = w_desc0, x_desc = x_desc0;
+                    if (++stage == p.ring.stages) {
+                        stage = 0, phase ^= 1, w_desc = w_desc0;
+                        if (!FEW) x_desc = x_desc0;
+                    }
                 }
-                tc_commit(&tmem_full[b]);
+                commit(smem_addr(&tmem_full[b]));
             }
         }
     } else {
         // ------------------------------ epilogue ------------------------------
         asm volatile("griddepcontrol.wait;" ::: "memory");
         const int quad = warp & 3;             // TMEM lane quadrant this warp may read
-        const int block = (warp - 2) >> 2;     // block of 128 vocabulary rows
-        const int tile_row = block * 128 + quad * 32;
+        // the four warps of a quadrant share the columns, 16 at a time, by twos where there are two blocks of 128 vocabulary rows
+        const int team = (warp - 2) >> 2, block = t.blocks == 2 ? team & 1 : 0;
+        const int c_first = 16 * (t.blocks == 2 ? team >> 1 : team), c_step = t.blocks == 2 ? 32 : 64;
+        const int tile_row = rank * t.w_box + block * 128 + quad * 32;
+        const int own_end = (rank + 1) * t.w_box;
+        float* scales = reinterpret_cast<float*>(fixed + 512);
+        float* turn = scales + 2 * 256 + (warp - 2) * 16 * kI8TurnStride;      // (STATS)
+        if constexpr (FEW) {
+            // this warp's part of its row, in 8 bits, to where the MMAs read it (tiles of N rows x 128 k, 128-byte swizzle)
+            const int team_warps = kI8EpiWarps / p.R, ew = warp - 2, row = ew / team_warps;
+            const bool mine = row < p.R;
+            const int first = ((ew - row * team_warps) * 32 + lane) * 8, stride = team_warps * 256;
+            const In* x = static_cast<const In*>(p.x) + row * p.ldx;
+            uint32_t* s_top = reinterpret_cast<uint32_t*>(scales + 256);
+            QuantChunk<In> c[kI8FewChunks];
+            uint32_t top_bits = 0u;
+#pragma unroll
+            for (int i = 0; i < kI8FewChunks; ++i)
+                if (mine && first + i * stride < p.d) c[i].load(x + first + i * stride);
+#pragma unroll
+            for (int i = 0; i < kI8FewChunks; ++i) {
+                if (!mine || first + i * stride >= p.d) continue;
+                float f[8];
+                c[i].get(f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top_bits = max(top_bits, __float_as_uint(f[j]) & 0x7fffffffu);
+            }
+            top_bits = __reduce_max_sync(kFullMask, top_bits);
+            if (lane == 0) s_top[ew] = top_bits;
+            named_barrier_sync(2, kI8EpiWarps * 32);
+            if (mine) {
+                for (int i = 0; i < team_warps; ++i) top_bits = max(top_bits, s_top[row * team_warps + i]);
+                const RowScale rs(top_bits);
+                if (first == 0) scales[row] = rs.scale;
+#pragma unroll
+                for (int i = 0; i < kI8FewChunks; ++i) {
+                    const int k = first + i * stride;
+                    if (k >= p.d) continue;
+                    float f[8];
+                    c[i].get(f);
+                    uint8_t* to = x_tiles + ((k >> 7) * t.N + row) * kI8BK + ((((k >> 4) & 7) ^ (row & 7)) << 4) + (k & 8);
+                    *reinterpret_cast<uint2*>(to) = rs.template round<In>(f);
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(rows_full);
+            named_barrier_sync(2, kI8EpiWarps * 32);
+        }
         int it = 0;
-        for (int item = blockIdx.x; item < items; item += gridDim.x, ++it) {
+        for (int item = worker; item < items; item += workers, ++it) {
             const int b = t.bufs == 2 ? it & 1 : 0;
             const int vt = item / t.MT, v0 = vt * t.TR, r0 = item % t.MT * t.NT;
-            const int vocab = min(t.TR, p.V - v0), rows = min(t.NT, p.R - r0);
+            const int vocab = min(PAIR ? own_end : t.TR, p.V - v0), rows = min(t.NT, p.R - r0);
             const int v = v0 + tile_row + lane;
             const bool in = tile_row + lane < vocab;
             const float ws = in ? __ldcg(p.w_scale + v) : 0.f;
+            // (from memory once for each item, while its products are made: in the loop below every other load would miss L1)
+            float* x_scale = FEW ? scales : scales + (it & 1) * 256;
+            if constexpr (!FEW) {
+                const int i = (int)threadIdx.x - 64;
+                if (i < rows) x_scale[i] = __ldcg(p.x_scale + r0 + i);
+                named_barrier_sync(2, kI8EpiWarps * 32);
+            }
             mbar_wait(&tmem_full[b], (t.bufs == 2 ? it >> 1 : it) & 1, p.status);
             tc_fence_after();
             if (tile_row < vocab) {
                 const uint32_t tmem = tmem_base + (b * t.blocks + block) * t.cols + (static_cast<uint32_t>(quad * 32) << 16);
-                Out* y = static_cast<Out*>(p.y) + (long long)r0 * p.ldy + v;
+                Out* y_tile = static_cast<Out*>(p.y) + (long long)r0 * p.ldy + v;
                 float2* stats = STATS ? p.stats + (long long)r0 * p.chunks + vt * (t.TR / kI8Chunk) + tile_row / kI8Chunk : nullptr;
 #pragma unroll 1
-                for (int c = 0; c < rows; c += 32) {
-                    float xs[32];      // (r0 + c is a multiple of 16)
+                for (int c = c_first; c < rows; c += c_step) {
+                    float z[16];
+                    {
+                        float xs[16];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 q = *reinterpret_cast<const float4*>(p.x_scale + r0 + c + 4 * i);
-                        xs[4 * i] = q.x, xs[4 * i + 1] = q.y, xs[4 * i + 2] = q.z, xs[4 * i + 3] = q.w;
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 q = *reinterpret_cast<const float4*>(x_scale + c + 4 * i);
+                            xs[4 * i] = q.x, xs[4 * i + 1] = q.y, xs[4 * i + 2] = q.z, xs[4 * i + 3] = q.w;
+                        }
+                        int acc[16];
+                        tmem_ld16(tmem + c, acc);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) z[i] = __fmul_rn(__fmul_rn(static_cast<float>(acc[i]), xs[i]), ws);
                     }
-                    float acc[32];
-                    tmem_ld32(tmem + c, acc);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) acc[i] = __fmul_rn(__fmul_rn(static_cast<float>(__float_as_int(acc[i])), xs[i]), ws);
                     if (in) {
+                        Out* y = y_tile + c * p.ldy;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (c + i < rows) store_logit(y, acc[i]);
+                        for (int i = 0; i < 16; ++i) {
+                            if (c + i < rows) store_logit(y, z[i]);
                             y += p.ldy;
                         }
                     }
                     if constexpr (STATS) {
-                        float2 mine = make_float2(0.f, 0.f);
-#pragma unroll
-                        for (int i = 0; i < 32; i += kI8StatsBatch) warp_chunk_stats<kI8StatsBatch>(acc + i, in, lane - i, mine);
-                        if (c + lane < rows) stats[(long long)(c + lane) * p.chunks] = mine;
+                        const float2 x = warp_chunk_stats(z, in, lane, turn);
+                        if (lane < 16 && c + lane < rows) stats[(long long)(c + lane) * p.chunks] = x;
                     }
                 }
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&tmem_empty[b]);
+            if (lane == 0) {
+                if constexpr (PAIR) mbar_arrive_cluster(leader_addr(smem_addr(&tmem_empty[b])));
+                else mbar_arrive(&tmem_empty[b]);
+            }
         }
     }
 
     tc_fence_before();
-    __syncthreads();
+    if constexpr (PAIR) cluster_sync();    // (neither CTA of a pair leaves before the other)
+    else __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, 512);
+        if constexpr (PAIR) tmem_dealloc_pair(tmem_base, 512);
+        else tmem_dealloc(tmem_base, 512);
     }
 }
 

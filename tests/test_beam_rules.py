@@ -14,23 +14,33 @@ int main() {
     const int grids[] = {1, 3, 147, 148}, vs[] = {1, 31, 128, 129, 300, 4000, 32000, 40011, 49152, 151936};
     for (int grid : grids)
         for (int V : vs)
-            for (int R = 1; R < 5000; R += R < 600 ? 1 : 61)
-                for (int chunks = 0; chunks < 2; ++chunks) {
-                    const Int8Tiling t = Int8Tiling::make(R, V, grid, chunks);
-                    bool ok = t.NT >= 1 && t.N >= t.NT && t.N % 16 == 0 && t.N <= 256 && (long long)t.MT * t.NT >= R && (long long)(t.MT - 1) * t.NT < R;
-                    ok = ok && t.TR >= 1 && t.TR <= 256 && t.TR <= 128 * t.blocks && (long long)t.NV * t.TR >= V && (long long)(t.NV - 1) * t.TR < V;
-                    ok = ok && (!chunks || t.TR % kI8Chunk == 0);
+            for (int R = 1; R < 5000; R += R < 300 ? 1 : 61)
+                for (int kind = 0; kind < 4; ++kind) {
+                    const bool chunks = kind & 1, pairs = kind & 2;
+                    if (pairs && grid < 2) continue;
+                    const int ctas = pairs ? 2 : 1;
+                    const Int8Tiling t = Int8Tiling::make(R, V, grid, chunks, pairs);
+                    bool ok = t.NT >= 1 && t.N >= t.NT && t.N % (16 * ctas) == 0 && t.N <= 256 && (long long)t.MT * t.NT >= R && (long long)(t.MT - 1) * t.NT < R;
+                    ok = ok && t.TR >= 1 && t.TR <= 256 && t.w_box <= 128 * t.blocks && t.w_box * ctas == t.TR && (long long)t.NV * t.TR >= V && (long long)(t.NV - 1) * t.TR < V;
+                    ok = ok && (!chunks || t.w_box % kI8Chunk == 0);
                     // accumulators of all buffers, as columns of tensor memory; reads of 32 columns end inside theirs
                     ok = ok && t.bufs * t.blocks * t.cols <= 512 && t.cols >= t.N && t.cols % 32 == 0 && t.NT % 16 == 0;
-                    const Int8Ring r = Int8Ring::make(t, 227 * 1024);
-                    ok = ok && r.stages >= 2 && r.stages <= kI8MaxStages && kI8FixedSmem + r.bytes <= 227 * 1024;
-                    ok = ok && r.w_bytes % 1024 == 0 && r.x_bytes % 1024 == 0 && r.w_bytes >= t.TR * kI8BK;
+                  for (int d : {8, 136, 768, 5120, 6144, 16384}) {
+                    const bool few = !pairs && Int8Ring::few(R, d);
+                    const Int8Ring r = Int8Ring::make(t, d, 227 * 1024 - kI8TurnBytes, few);
+                    ok = ok && r.stages >= 2 && r.stages <= kI8MaxStages && kI8FixedSmem + kI8TurnBytes + r.bytes + r.resident <= 227 * 1024;
+                    ok = ok && r.w_bytes % 1024 == 0 && r.x_bytes % 1024 == 0 && r.w_bytes >= t.w_box * kI8BK;
+                    // the hidden-row boxes of a tile are what its MMA takes, or all there are
+                    ok = ok && (pairs ? 2 * t.x_box == t.N : t.x_box == t.N || (t.x_box >= R && t.x_box % 8 == 0));
+                    if (few) { ok = ok && R <= kI8EpiWarps && t.MT == 1 && r.resident >= (d + 127) / 128 * 128 * t.N && r.resident % 1024 == 0; }
+                    else ok = ok && r.x_bytes * ctas >= t.N * kI8BK;
                     // what the last stage's MMAs read
                     ok = ok && (r.stages - 1) * r.w_bytes + t.blocks * 128 * kI8BK <= r.bytes && r.stages * (r.w_bytes + r.x_bytes) <= r.bytes;
+                  }
                     // no more rounds of items than whole tiles of 256 need
                     const long long whole = (long long)t.MT * ((V + 255) / 256);
-                    ok = ok && ((long long)t.MT * t.NV + grid - 1) / grid <= (whole + grid - 1) / grid;
-                    if (!ok) return std::printf("R %d V %d grid %d chunks %d\n", R, V, grid, chunks), 1;
+                    ok = ok && ((long long)t.MT * t.NV + grid / ctas - 1) / (grid / ctas) <= (whole + grid / ctas - 1) / (grid / ctas);
+                    if (!ok) return std::printf("R %d V %d grid %d kind %d\n", R, V, grid, kind), 1;
                 }
     return 0;
 }
