@@ -84,14 +84,14 @@ int check_head(const disco_ctx* c, const int8_t* W_q, long long ldw, const float
 
 // The product of hidden rows that are in 8 bits already (In = void), or of a few rows of type In.
 template <typename Out, typename In, bool STATS, bool PAIR>
-int launch_int8_head(disco_ctx* c, const int8_t* W_q, long long ldw, const float* w_scale, const void* x, long long ldx, int d, int R, void* y,
-                     long long ldy, cudaStream_t st) {
+int launch_int8_head(disco_ctx* c, const Int8Tiling& t, const int8_t* W_q, long long ldw, const float* w_scale, const void* x, long long ldx,
+                     int d, int R, void* y, long long ldy, cudaStream_t st) {
     constexpr bool FEW = !std::is_void<In>::value;
     Int8Params p{};
     p.V = c->V;
     p.d = d;
     p.R = R;
-    p.t = Int8Tiling::make(R, c->V, c->sm_count, STATS, PAIR);
+    p.t = t;
     p.w_scale = w_scale;
     p.x_scale = c->int8_scale;
     p.x = x;
@@ -129,19 +129,18 @@ int launch_int8_head(disco_ctx* c, const int8_t* W_q, long long ldw, const float
 template <typename Out, bool STATS>
 int project(disco_ctx* c, const int8_t* W_q, long long ldw, const float* w_scale, const void* H, int h_type, long long ldh, int d, int R, void* y,
             long long ldy, cudaStream_t st) {
+    const Int8Tiling t = Int8Tiling::choose(R, c->V, d, c->sm_count);
     if (Int8Ring::few(R, d)) {
         switch (h_type) {
-            case DISCO_F32: return launch_int8_head<Out, float, STATS, false>(c, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
-            case DISCO_BF16: return launch_int8_head<Out, __nv_bfloat16, STATS, false>(c, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
-            default: return launch_int8_head<Out, __half, STATS, false>(c, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
+            case DISCO_F32: return launch_int8_head<Out, float, STATS, false>(c, t, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
+            case DISCO_BF16: return launch_int8_head<Out, __nv_bfloat16, STATS, false>(c, t, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
+            default: return launch_int8_head<Out, __half, STATS, false>(c, t, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
         }
     }
     const int rc = quantize(c, H, h_type, ldh, R, d, c->int8_rows, c->int8_pitch, c->int8_scale, st);
     if (rc) return rc;
-    static const char* e = getenv("I8PAIR");
-    const bool pair = e ? atoi(e) : R > 128;
-    return pair ? launch_int8_head<Out, void, STATS, true>(c, W_q, ldw, w_scale, nullptr, 0, d, R, y, ldy, st)
-                : launch_int8_head<Out, void, STATS, false>(c, W_q, ldw, w_scale, nullptr, 0, d, R, y, ldy, st);
+    return t.kind == kI8Pair ? launch_int8_head<Out, void, STATS, true>(c, t, W_q, ldw, w_scale, nullptr, 0, d, R, y, ldy, st)
+                             : launch_int8_head<Out, void, STATS, false>(c, t, W_q, ldw, w_scale, nullptr, 0, d, R, y, ldy, st);
 }
 
 int check_beams(const disco_ctx* c, int B, int K, int n, const float* score, const uint8_t* finished, int eos, const float* score_out,

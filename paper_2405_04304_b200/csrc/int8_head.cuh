@@ -7,7 +7,6 @@
 // the sum, times s_x, times s_w.
 #pragma once
 
-#include <cstdlib>
 #include <type_traits>
 
 #include <cuda_bf16.h>
@@ -166,42 +165,64 @@ constexpr int kI8FixedSmem = 1024 /*align*/ + 512 /*barriers*/ + 2 * 256 * 4 /*s
 
 __host__ __device__ inline int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
-// How V vocabulary rows and R hidden rows are cut: MT tiles of NT hidden rows (the columns of an accumulator; the MMA takes N of
-// them) times NV tiles of TR vocabulary rows (one or two blocks of 128 TMEM lanes).  Item i is hidden tile i % MT of vocabulary tile
-// i / MT; the CTAs take items in turn, so those that share a vocabulary tile run side by side and the head crosses HBM once.
-//
-// Pairs of CTAs (cta_group::2): a tile's vocabulary rows lie half in each CTA (one block), and so do the hidden rows that both multiply by.
+// How V vocabulary rows and R hidden rows are cut: MT tiles of N hidden rows (the columns of an accumulator) times NV tiles of TR
+// vocabulary rows.  Item i is hidden tile i % MT of vocabulary tile i / MT; the workers take items in turn, so those that share a
+// vocabulary tile run side by side and the head crosses HBM once.  TR is a multiple of 32: whole lines of y, whole chunks.
+//   one    a CTA is a worker, TR <= 128: one block of TMEM lanes, two accumulators, the epilogue under the next item's products
+//   two    TR <= 256, two blocks: fewer reads of the hidden rows; beyond 128 hidden rows one accumulator only
+//   pair   two CTAs are a worker (cta_group::2), TR <= 256: half of the vocabulary rows lie in each, and half of the hidden rows that both
+//          multiply by; two accumulators
+enum Int8Kind { kI8One, kI8Two, kI8Pair };
 struct Int8Tiling {
-    int MT, NT, N, NV, TR, blocks, cols, bufs;
+    int MT, N, NV, TR, blocks, cols, bufs;
     int w_box, x_box;      // rows of the boxes that a CTA loads
-    __host__ __device__ static Int8Tiling make(int R, int V, int grid, bool whole_chunks, bool pairs) {
+    Int8Kind kind;
+    int rounds;            // items to a worker at most
+    __host__ __device__ static Int8Tiling make(int R, int V, int grid, Int8Kind kind) {
         Int8Tiling t;
-        const int ctas = pairs ? 2 : 1;
+        const int ctas = kind == kI8Pair ? 2 : 1, most_rows = kind == kI8One ? 128 : 256;
+        t.kind = kind;
         t.MT = (R + 255) / 256;
-#ifndef __CUDA_ARCH__
-        if (getenv("I8MT")) t.MT += atoi(getenv("I8MT"));
-#endif
         t.N = round_up((R + t.MT - 1) / t.MT, 16 * ctas);
-        t.NT = t.N;
-        t.MT = (R + t.NT - 1) / t.NT;
-        // as few rounds of items as tiles of 256 vocabulary rows need, all items alike
+        t.MT = (R + t.N - 1) / t.N;
+        // as few rounds of items as the largest tiles need, all items alike
         const int workers = grid / ctas;
-        const long long items = (long long)t.MT * ((V + 255) / 256);
+        const long long items = (long long)t.MT * ((V + most_rows - 1) / most_rows);
         const long long rounds = (items + workers - 1) / workers;
         const long long most = rounds * workers / t.MT;
         const int nv = (int)(most < V ? (most > 1 ? most : 1) : V);
-        t.TR = round_up((V + nv - 1) / nv, ctas * (whole_chunks ? kI8Chunk : 1));
-        if (t.TR > 256) t.TR = 256;
-#ifndef __CUDA_ARCH__
-        if (getenv("I8TR")) t.TR = atoi(getenv("I8TR"));
-#endif
+        t.TR = round_up((V + nv - 1) / nv, kI8Chunk * ctas);
+        // (a tile of many hidden rows is worth reading for whole blocks only: 200 rows of 8000 x 2048 / 12000 x 5120, 55 / 82 -> 128
+        // vocabulary rows to a CTA, 13.4 / 26.1 -> 12.7 / 23.9 us)
+        if (R > 96 && rounds == 1 && t.TR < 128 * ctas) t.TR = 128 * ctas;
+        if (t.TR > most_rows) t.TR = most_rows;
         t.NV = (V + t.TR - 1) / t.TR;
-        t.blocks = t.TR > 128 && !pairs ? 2 : 1;
+        t.rounds = (int)(((long long)t.MT * t.NV + workers - 1) / workers);
+        t.blocks = t.TR > 128 && kind == kI8Two ? 2 : 1;
         t.cols = round_up(t.N, 32);
         t.bufs = 2 * t.blocks * t.cols <= 512 ? 2 : 1;
         t.w_box = t.TR / ctas;
-        t.x_box = pairs ? t.N / 2 : (round_up(R, 8) < t.N ? round_up(R, 8) : t.N);
+        t.x_box = ctas == 2 ? t.N / 2 : (round_up(R, 8) < t.N ? round_up(R, 8) : t.N);
         return t;
+    }
+    // The kind, from passes of 11 to 704 rows of heads of 8000 x 2048 to 49152 x 2048 and 32000 x 5120 (us, one / two / pair):
+    //   * up to 32 hidden rows the epilogue is short and HBM is the bound: two (32000 x 5120, 11 rows 31.2 / 30.3 / 31.4)
+    //   * beyond, it pays to have it under the next item's products: one (32000 x 768, 64 / 200 / 300 rows 10.0 / 15.0 / 16.9, 12.0 / 17.2 /
+    //     18.1, 12.4 / 17.4 / 20.8)
+    //   * long contractions of many rows are bound by the operands' way from L2: pair (32000 x 5120, 128 / 200 / 256 / 320 rows 36.8 / 45.1 /
+    //     53.4 / 63.0, 36.7 / 45.0 / 52.8 / 60.9, 36.1 / 42.3 / 48.7 / 59.2)
+    // unless it leaves a CTA more vocabulary rows, rounds counted, by over 15 % (200 rows of 20000 x 3000: 2 x 96 for one and pair, 160 for
+    // two: 26.7 / 22.8 / 24.5).
+    __host__ __device__ int share() const { return rounds * w_box; }
+    __host__ __device__ static Int8Tiling choose(int R, int V, int d, int grid) {
+        const Int8Tiling two = make(R, V, grid, kI8Two);
+        if (R <= 32) return two;
+        const Int8Tiling one = make(R, V, grid, kI8One);
+        const bool spread = 100 * one.share() > 115 * two.share();
+        const Int8Tiling single = spread ? two : one;
+        if (R <= 96 || d < 2048 || grid < 2) return single;
+        const Int8Tiling pair = make(R, V, grid, kI8Pair);
+        return 100 * pair.share() > 115 * single.share() ? single : pair;
     }
 };
 
@@ -407,11 +428,11 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
             }
             if (!FEW) asm volatile("griddepcontrol.wait;" ::: "memory");
             asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-            for (int n = 0; !FEW && n < pre; ++n) load(x0 + n * p.ring.x_bytes, &tmap_X, n * kI8BK, item % t.MT * t.NT + r_own, n);
+            for (int n = 0; !FEW && n < pre; ++n) load(x0 + n * p.ring.x_bytes, &tmap_X, n * kI8BK, item % t.MT * t.N + r_own, n);
             int stage = pre == p.ring.stages ? 0 : pre, phase = pre == p.ring.stages ? 1 : 0;
             int k = pre * kI8BK;
             for (; item < items; item += workers, k = 0) {
-                const int v0 = item / t.MT * t.TR + v_own, r0 = item % t.MT * t.NT + r_own;
+                const int v0 = item / t.MT * t.TR + v_own, r0 = item % t.MT * t.N + r_own;
                 for (; k < k_end; k += kI8BK) {
                     mbar_wait(empty0 + stage * 8, phase ^ 1, p.status);
                     if (leader) mbar_arrive_expect_tx(full0 + stage * 8, expected);
@@ -534,8 +555,8 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
         int it = 0;
         for (int item = worker; item < items; item += workers, ++it) {
             const int b = t.bufs == 2 ? it & 1 : 0;
-            const int vt = item / t.MT, v0 = vt * t.TR, r0 = item % t.MT * t.NT;
-            const int vocab = min(PAIR ? own_end : t.TR, p.V - v0), rows = min(t.NT, p.R - r0);
+            const int vt = item / t.MT, v0 = vt * t.TR, r0 = item % t.MT * t.N;
+            const int vocab = min(PAIR ? own_end : t.TR, p.V - v0), rows = min(t.N, p.R - r0);
             const int v = v0 + tile_row + lane;
             const bool in = tile_row + lane < vocab;
             const float ws = in ? __ldcg(p.w_scale + v) : 0.f;

@@ -15,16 +15,16 @@ int main() {
     for (int grid : grids)
         for (int V : vs)
             for (int R = 1; R < 5000; R += R < 300 ? 1 : 61)
-                for (int kind = 0; kind < 4; ++kind) {
-                    const bool chunks = kind & 1, pairs = kind & 2;
+                for (int kind = 0; kind < 3; ++kind) {
+                    const bool pairs = kind == kI8Pair;
                     if (pairs && grid < 2) continue;
                     const int ctas = pairs ? 2 : 1;
-                    const Int8Tiling t = Int8Tiling::make(R, V, grid, chunks, pairs);
-                    bool ok = t.NT >= 1 && t.N >= t.NT && t.N % (16 * ctas) == 0 && t.N <= 256 && (long long)t.MT * t.NT >= R && (long long)(t.MT - 1) * t.NT < R;
+                    const Int8Tiling t = Int8Tiling::make(R, V, grid, (Int8Kind)kind);
+                    bool ok = t.N % (16 * ctas) == 0 && t.N >= 16 && t.N <= 256 && (long long)t.MT * t.N >= R && (long long)(t.MT - 1) * t.N < R;
                     ok = ok && t.TR >= 1 && t.TR <= 256 && t.w_box <= 128 * t.blocks && t.w_box * ctas == t.TR && (long long)t.NV * t.TR >= V && (long long)(t.NV - 1) * t.TR < V;
-                    ok = ok && (!chunks || t.w_box % kI8Chunk == 0);
+                    ok = ok && t.w_box % kI8Chunk == 0 && (long long)t.rounds * (grid / ctas) >= (long long)t.MT * t.NV;
                     // accumulators of all buffers, as columns of tensor memory; reads of 32 columns end inside theirs
-                    ok = ok && t.bufs * t.blocks * t.cols <= 512 && t.cols >= t.N && t.cols % 32 == 0 && t.NT % 16 == 0;
+                    ok = ok && t.bufs * t.blocks * t.cols <= 512 && t.cols >= t.N && t.cols % 32 == 0;
                   for (int d : {8, 136, 768, 5120, 6144, 16384}) {
                     const bool few = !pairs && Int8Ring::few(R, d);
                     const Int8Ring r = Int8Ring::make(t, d, 227 * 1024 - kI8TurnBytes, few);
@@ -37,11 +37,20 @@ int main() {
                     // what the last stage's MMAs read
                     ok = ok && (r.stages - 1) * r.w_bytes + t.blocks * 128 * kI8BK <= r.bytes && r.stages * (r.w_bytes + r.x_bytes) <= r.bytes;
                   }
-                    // no more rounds of items than whole tiles of 256 need
-                    const long long whole = (long long)t.MT * ((V + 255) / 256);
-                    ok = ok && ((long long)t.MT * t.NV + grid / ctas - 1) / (grid / ctas) <= (whole + grid / ctas - 1) / (grid / ctas);
+                    // no more rounds of items than the largest tiles need
+                    const int most = kind == kI8One ? 128 : 256, workers = grid / ctas;
+                    const long long whole = (long long)t.MT * ((V + most - 1) / most);
+                    ok = ok && t.rounds <= (whole + workers - 1) / workers;
                     if (!ok) return std::printf("R %d V %d grid %d kind %d\n", R, V, grid, kind), 1;
                 }
+    // which kind is taken, at sizes where all three were measured
+    struct { int R, V, d, kind; } taken[] = {{11, 32000, 5120, kI8Two}, {24, 49152, 2048, kI8Two}, {64, 32000, 768, kI8One}, {200, 32000, 768, kI8One},
+        {300, 32000, 768, kI8One}, {200, 32000, 5120, kI8Pair}, {256, 32000, 5120, kI8Pair}, {320, 32000, 5120, kI8Pair}, {704, 32000, 5120, kI8Pair},
+        {256, 49152, 2048, kI8Pair}, {200, 20000, 3000, kI8Two}, {200, 12000, 5120, kI8Pair}, {100, 40011, 1000, kI8One}};
+    for (auto& m : taken) {
+        const Int8Tiling t = Int8Tiling::choose(m.R, m.V, m.d, 148);
+        if (t.kind != m.kind) return std::printf("kind: %d rows, %d x %d: %d\n", m.R, m.V, m.d, t.kind), 1;
+    }
     return 0;
 }
 """
