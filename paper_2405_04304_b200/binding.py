@@ -6,8 +6,8 @@ and streams only); the ``*_host`` calls take CPU tensors (pinned for asynchronou
 """
 from __future__ import annotations
 
+import array
 import ctypes
-import math
 import os
 
 import torch
@@ -469,25 +469,33 @@ class Context:
         if count == 0 or count != len(dst) or parent.dim() != 2:
             raise ValueError("expected as many states in dst as in src, and parent [B, n]")
         B, n = parent.shape
-        shape, dtype, device = src[0].shape, src[0].dtype, self.device
+        first, device = src[0], self.device
+        shape, dtype = first.shape, first.dtype
         rows, inner = shape[0], shape[1:]
         if B == 0 or rows == 0 or rows % B or not 1 <= length_dim <= len(shape):
             raise ValueError(f"{rows} rows are no beams of {B} sequences, or there is no dimension {length_dim}")
         if lens is not None and (length_dim == len(shape) or lens.numel() != B):
             raise ValueError(f"expected {B} lengths along one of the states' dimensions")
-        ptrs = []
-        for states, expected in ((src, shape), (dst, torch.Size((B * n,) + inner))):
+        ptrs = array.array("Q")
+        for states, expected in ((src, shape), (dst, torch.Size((B * n, *inner)))):
             for t in states:
                 if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.shape != expected:
                     raise ValueError(f"expected contiguous {dtype} states {tuple(expected)} on cuda:{device}, got {t.dtype} {tuple(t.shape)}")
                 ptrs.append(t.data_ptr())
-        mid = math.prod(inner[:length_dim - 1])
-        T = inner[length_dim - 1] if length_dim <= len(inner) else 1
-        unit = math.prod(inner[length_dim:]) * src[0].element_size()
-        array = ctypes.c_void_p * count
+        # [rows, mid, T, unit]
+        mid = T = 1
+        unit = first.element_size()
+        for i, size in enumerate(inner, 1):
+            if i < length_dim:
+                mid *= size
+            elif i == length_dim:
+                T = size
+            else:
+                unit *= size
+        at = ptrs.buffer_info()[0]
         rc = self._lib.disco_beam_reorder(
-            self._h, array(*ptrs[:count]), array(*ptrs[count:]), count, B, rows // B, n, self._on(parent, torch.int32),
-            self._on(lens, torch.int32), mid, T, unit, self._here(stream))
+            self._h, at, at + 8 * count, count, B, rows // B, n, self._on(parent, torch.int32), self._on(lens, torch.int32), mid, T,
+            unit, self._here(stream))
         if rc != OK:
             raise DiscoError(rc, "disco_beam_reorder")
 

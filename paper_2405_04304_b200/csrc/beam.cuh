@@ -2,8 +2,8 @@
 //
 // Selection.  Of a sequence with K beams of score c_k and logits z_k[v], the n best continuations by
 //     l[k, v] = c_k + z_k[v] - ln sum_w exp z_k[w],      ties to the lowest (k, v).
-// Every logit is read once, by a pass that leaves two numbers for each chunk of neighbouring logits: the largest, and the sum of
-// exp(z - largest).  (The 8-bit LM head's epilogue leaves the same.)  What follows looks at few logits: the n best lie in the n chunks
+// Every logit is read once, by a pass that leaves the largest of each chunk of neighbouring logits, and sums of exponentials.  (The 8-bit LM
+// head's epilogue leaves the same.)  What follows looks at few logits: the n best lie in the n chunks
 // that come first by (best score, place), since each of those holds a candidate that beats whatever lies in
 // another chunk.  Scores are formed and compared in 64 bits: which of two candidates is the better is a whole number, and the scores of
 // different beams may come as near to each other as they like.
@@ -42,9 +42,10 @@ struct BeamDeal {
         d.used = (d.pieces + d.share * 32 - 1) / (d.share * 32);
         return d;
     }
-    // Warps: as few of 8, 16 and 32 as hold every chunk as a piece of its own, otherwise 32.
-    __host__ __device__ static int warps(int K, int chunks) {
-        for (int w = 8; w < 32; w *= 2)
+    // Warps: as few of 8, 16 and 32 as hold every chunk as a piece of its own, otherwise 32; more where many are kept, since step 3 reads
+    // about as many pieces.
+    __host__ __device__ static int warps(int K, int chunks, int n) {
+        for (int w = n <= 10 ? 8 : n <= 24 ? 16 : 32; w < 32; w *= 2)
             if (K <= w && make(K, chunks, w).merged == 1) return w;
         return 32;
     }
@@ -57,8 +58,10 @@ struct BeamParams {
     int eos;                     // the continuation of a finished beam (-1: none)
     const float* score;          // [B, K]
     const uint8_t* finished;     // [B, K] or null
-    float2* stats;               // [B * K][chunks]
-    int chunks;
+    int chunks, segs;
+    float* tops;                 // [B * K][chunks] largest logits of chunks of kBeamChunk
+    float2* sums;                // [B * K][segs] of kBeamWarpChunks chunks each: their largest logit, the sum of exp(z - largest)
+    const float2* pairs;         // [B * K][chunks] both for each chunk of kI8Chunk (instead of tops and sums)
     BeamDeal deal;
     float* score_out;            // [B, n]
     int32_t* parent;
@@ -73,6 +76,16 @@ __device__ __forceinline__ float load_logit(const __nv_bfloat16* p) {
 __device__ __forceinline__ float load_logit(const __half* p) {
     return __half2float(__ushort_as_half(__ldcg(reinterpret_cast<const unsigned short*>(p))));
 }
+__device__ __forceinline__ void load_logits2(const __nv_bfloat16* p, float& a, float& b) {
+    const uint32_t q = __ldcg(reinterpret_cast<const uint32_t*>(p));
+    a = __uint_as_float(q << 16), b = __uint_as_float(q & 0xffff0000u);
+}
+__device__ __forceinline__ void load_logits2(const __half* p, float& a, float& b) {
+    const uint32_t q = __ldcg(reinterpret_cast<const uint32_t*>(p));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&q));
+    a = f.x, b = f.y;
+}
+
 // Does the row's beam take part, and by its logits?
 __device__ __forceinline__ bool beam_lives(float c) { return c > DISCO_NEG_INF && c < -DISCO_NEG_INF; }
 __device__ __forceinline__ bool beam_expands(const BeamParams& p, int row) {
@@ -80,41 +93,79 @@ __device__ __forceinline__ bool beam_expands(const BeamParams& p, int row) {
 }
 
 // The pass over the logits.  A warp takes eight chunks of a row; which lane holds which logit goes by its index alone, so that equal
-// rows give equal sums wherever they lie.
+// rows give equal sums wherever they lie.  (The eight chunks' largest logits meet in nine exchanges, each lane keeping half of what it has
+// at each of the first three; with two reductions over the warp for each chunk the pass over bf16 logits took as long as over twice as many
+// bytes of fp32.)
 template <typename T>
 __global__ void __launch_bounds__(kBeamStatWarps * 32) beam_stats_kernel(const BeamParams p) {
+    static_assert(kBeamWarpChunks == 8, "three halvings");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const long long w = (long long)blockIdx.x * kBeamStatWarps + (threadIdx.x >> 5);
-    const int per_row = (p.chunks + kBeamWarpChunks - 1) / kBeamWarpChunks;
-    const long long row = w / per_row;
+    const long long row = w / p.segs;
     if (row >= (long long)p.B * p.K) return;
     if (!beam_expands(p, (int)row)) return;
-    const int first = (int)(w % per_row) * kBeamWarpChunks;
-    const int v0 = first * kBeamChunk + lane;
-    const T* z = static_cast<const T*>(p.z) + row * p.ld;
+    const int seg = (int)(w % p.segs), first = seg * kBeamWarpChunks;
+    // a lane's logits of a chunk: two by two neighbours of 16 bits, so that they can be loaded together, every 32nd of 32 bits
+    constexpr int kNext = sizeof(T) == 2 ? 2 : 1;
+    const int v0 = first * kBeamChunk + lane * kNext;
+    const T* z = static_cast<const T*>(p.z) + row * p.ld + v0;
     float f[kBeamWarpChunks][4];
+    const bool whole = (first + kBeamWarpChunks) * kBeamChunk <= p.V;
+    if (whole && (kNext == 1 || (reinterpret_cast<uintptr_t>(z) & 3) == 0)) {
 #pragma unroll
-    for (int c = 0; c < kBeamWarpChunks; ++c)
+        for (int c = 0; c < kBeamWarpChunks; ++c) {
+            if constexpr (kNext == 2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int v = v0 + c * kBeamChunk + i * 32;
-            f[c][i] = v < p.V ? load_logit(z + v) : DISCO_NEG_INF;
+                for (int i = 0; i < 2; ++i) load_logits2(z + c * kBeamChunk + i * 64, f[c][2 * i], f[c][2 * i + 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[c][i] = load_logit(z + c * kBeamChunk + i * 32);
+            }
         }
-    float2 mine = make_float2(0.f, 0.f);
+    } else {
 #pragma unroll
-    for (int c = 0; c < kBeamWarpChunks; ++c) {
-        const float m = warp_max_nan_f32(max_nan(max_nan(f[c][0], f[c][1]), max_nan(f[c][2], f[c][3])));
-        uint32_t e = 0u;
-        if (m > DISCO_NEG_INF && m < -DISCO_NEG_INF) {
-            const float s = (__expf(f[c][0] - m) + __expf(f[c][1] - m)) + (__expf(f[c][2] - m) + __expf(f[c][3] - m));
-            e = __float2uint_rn(s * 0x1p24f);   // (128 terms of at most 1)
-        }
-        const float s = static_cast<float>(__reduce_add_sync(kFullMask, e)) * 0x1p-24f;
-        if (lane == c) mine = make_float2(m, s);
+        for (int c = 0; c < kBeamWarpChunks; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = c * kBeamChunk + (kNext == 2 ? (i >> 1) * 64 + (i & 1) : i * 32);
+                f[c][i] = v0 + at < p.V ? load_logit(z + at) : DISCO_NEG_INF;
+            }
     }
-    if (lane < kBeamWarpChunks && first + lane < p.chunks) p.stats[row * p.chunks + first + lane] = mine;
+    float t[kBeamWarpChunks];
+#pragma unroll
+    for (int c = 0; c < kBeamWarpChunks; ++c) t[c] = max_nan(max_nan(f[c][0], f[c][1]), max_nan(f[c][2], f[c][3]));
+#pragma unroll
+    for (int half = 4; half >= 1; half >>= 1) {      // lanes apart by 4 * half
+        const bool up = lane & (4 * half);
+#pragma unroll
+        for (int c = 0; c < half; ++c) {
+            const float keep = up ? t[c + half] : t[c], send = up ? t[c] : t[c + half];
+            t[c] = max_nan(keep, __shfl_xor_sync(kFullMask, send, 4 * half));
+        }
+    }
+    t[0] = max_nan(t[0], __shfl_xor_sync(kFullMask, t[0], 2));
+    t[0] = max_nan(t[0], __shfl_xor_sync(kFullMask, t[0], 1));      // chunk lane / 4
+    const float m = warp_max_nan_f32(t[0]);
+    float s[kBeamWarpChunks];
+    const bool serves = ExpFrom::serves(m);
+    const ExpFrom from(m);
+    if (serves) {
+#pragma unroll
+        for (int c = 0; c < kBeamWarpChunks; ++c) s[c] = (from(f[c][0]) + from(f[c][1])) + (from(f[c][2]) + from(f[c][3]));
+    } else {
+#pragma unroll
+        for (int c = 0; c < kBeamWarpChunks; ++c) s[c] = (__expf(f[c][0] - m) + __expf(f[c][1] - m)) + (__expf(f[c][2] - m) + __expf(f[c][3] - m));
+    }
+#pragma unroll
+    for (int half = 4; half >= 1; half >>= 1)
+#pragma unroll
+        for (int c = 0; c < half; ++c) s[c] += s[c + half];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) s[0] += __shfl_xor_sync(kFullMask, s[0], off);
+    if ((lane & 3) == 0 && first + (lane >> 2) < p.chunks) p.tops[row * p.chunks + first + (lane >> 2)] = t[0];
+    if (lane == 0) p.sums[row * p.segs + seg] = make_float2(m, serves ? from.sum(s[0], m) : s[0]);      // (no number where the largest is not finite: nothing is done with it)
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -179,9 +230,9 @@ __device__ __forceinline__ void block_cut(Reach reach, unsigned long long lo, un
 template <typename T, int CHUNK, int THREADS>
 __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p) {
     constexpr int kWarps = THREADS / 32;
-    __shared__ unsigned long long s_key[kBeamList];
-    __shared__ long long s_place[kBeamList];
+    __shared__ ulonglong2 s_cand[kBeamList];      // (score, place); in step 3 the logit's bits for the score
     __shared__ int2 s_piece[kBeamPieceList];
+    __shared__ float s_piece_top[kBeamPieceList];
     __shared__ int s_sum[2][32];
     __shared__ float s_max[2][32];
     __shared__ double s_exp[2][32];
@@ -189,7 +240,7 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     __shared__ float s_score[kBeamMaxBeams], s_top[kBeamMaxBeams], s_offset[kBeamMaxBeams], s_err[kBeamMaxBeams];
     __shared__ int s_state[kBeamMaxBeams];      // 0: no continuation, 1: expands, 2: finished
     __shared__ int s_pieces, s_count;
-    __shared__ uint32_t s_best;
+    __shared__ uint32_t s_best[3];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -205,18 +256,40 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     float best[kBeamItems];
     {
         float m[2] = {DISCO_NEG_INF, DISCO_NEG_INF}, e[2] = {0.f, 0.f};
+        // a row's sums join those of this lane: relative to the larger of the largest logits
+        auto join = [&](int r, float top, float sum) {
+            if (!(top > DISCO_NEG_INF)) return;       // (NaN: the row's largest logit says so)
+            const float now = fmaxf(m[r], top);
+            e[r] = e[r] * __expf(m[r] - now) + sum * __expf(top - now);
+            m[r] = now;
+        };
+        if constexpr (CHUNK == kBeamChunk) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int k = warp_row + 32 * r;
+                if (k >= p.K || (r == 1 && !deal.two)) continue;
+                for (int i = warp_share * 32 + lane; i < p.segs; i += deal.share * 32) {
+                    const float2 x = __ldcg(p.sums + (long long)(b * p.K + k) * p.segs + i);
+                    join(r, x.x, x.y);
+                }
+            }
+        }
+        float top[2] = {DISCO_NEG_INF, DISCO_NEG_INF};
 #pragma unroll
         for (int j = 0; j < kBeamItems; ++j) best[j] = DISCO_NEG_INF;
 #pragma unroll 1
         for (int g = 0; g < deal.merged; ++g) {
             float2 x[kBeamItems];
-            float top[2] = {DISCO_NEG_INF, DISCO_NEG_INF};
 #pragma unroll
             for (int j = 0; j < kBeamItems; ++j) {
                 x[j] = make_float2(DISCO_NEG_INF, 0.f);
                 if (item_used(j)) {
                     const int k = item_row(j), piece = item_piece(j), chunk = piece * deal.merged + g;
-                    if (k < p.K && chunk < p.chunks && piece < deal.pieces) x[j] = __ldcg(p.stats + (long long)(b * p.K + k) * p.chunks + chunk);
+                    if (k < p.K && chunk < p.chunks && piece < deal.pieces) {
+                        const long long at = (long long)(b * p.K + k) * p.chunks + chunk;
+                        if constexpr (CHUNK == kBeamChunk) x[j].x = __ldcg(p.tops + at);
+                        else x[j] = __ldcg(p.pairs + at);
+                    }
                 }
             }
             if (g == 0) {
@@ -226,7 +299,8 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
                     s_score[tid] = c;
                     s_state[tid] = !beam_lives(c) ? 0 : over ? 2 : 1;
                 }
-                if (tid == 0) s_count = 0, s_pieces = 0, s_best = 0u;
+                if (tid < 3) s_best[tid] = 0u;
+                if (tid == 0) s_count = 0, s_pieces = 0;
             }
 #pragma unroll
             for (int j = 0; j < kBeamItems; ++j) {
@@ -236,15 +310,27 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
                 top[0] = max_nan(top[0], r ? DISCO_NEG_INF : x[j].x);
                 top[1] = max_nan(top[1], r ? x[j].x : DISCO_NEG_INF);
             }
+            if constexpr (CHUNK != kBeamChunk) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    if (r == 1 && !deal.two) continue;
+                    const float now = warp_max_nan_f32(top[r]);
+                    if (now > m[r]) e[r] *= __expf(m[r] - now);
+                    m[r] = now;
+#pragma unroll
+                    for (int j = 0; j < kBeamItems; ++j)
+                        if (item_used(j) && (deal.two && j >= kHalf) == (r == 1) && x[j].x > DISCO_NEG_INF)
+                            e[r] = fmaf(x[j].y, __expf(x[j].x - now), e[r]);
+                }
+            }
+        }
+        if constexpr (CHUNK == kBeamChunk) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 if (r == 1 && !deal.two) continue;
-                const float now = max_nan(m[r], warp_max_nan_f32(top[r]));
-                if (now > m[r]) e[r] *= m[r] > DISCO_NEG_INF ? __expf(m[r] - now) : 0.f;
+                const float now = warp_max_nan_f32(max_nan(m[r], top[r]));
+                e[r] = m[r] > DISCO_NEG_INF ? e[r] * __expf(m[r] - now) : 0.f;
                 m[r] = now;
-#pragma unroll
-                for (int j = 0; j < kBeamItems; ++j)
-                    if (item_used(j) && (deal.two && j >= kHalf) == (r == 1) && x[j].x > DISCO_NEG_INF) e[r] = fmaf(x[j].y, __expf(x[j].x - now), e[r]);
             }
         }
 #pragma unroll
@@ -298,17 +384,18 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         if (best[j] > DISCO_NEG_INF && f < -DISCO_NEG_INF) low = fmaxf(low, f - e);       // (beyond what fp32 holds: no bound)
         high[j] = f + e;
     }
-    // The n-th largest of these bounds, or a little less.  Each step costs a barrier that counts, so the search goes out from the largest
-    // one, in strides that grow until n reach it, and only then halves what is left.
-    {
+    // The n-th largest of the threads' bounds, or a little less.  Each step costs a barrier that counts, so the search goes out from the
+    // largest one, in strides that grow until n reach it, and only then halves what is left.
+    auto find_floor = [&](float low, int use) {
         const uint32_t key = ordered_bits(low), top = __reduce_max_sync(kFullMask, key);
-        if (lane == 0) atomicMax(&s_best, top);
+        if (lane == 0) atomicMax(&s_best[use], top);
         __syncthreads();
-        uint32_t lo = 0u, hi = s_best + 1u, stride = 1u << 18;       // reached by n, and by fewer
+        const uint32_t best = s_best[use];
+        uint32_t lo = 0u, hi = best + 1u, stride = 1u << 18;       // reached by n, and by fewer
         bool out = true;
 #pragma unroll 1
         while (hi - lo > 1u) {
-            const uint32_t at = out ? (s_best > stride ? s_best - stride : 0u) : lo + (hi - lo) / 2;
+            const uint32_t at = out ? (best > stride ? best - stride : 0u) : lo + (hi - lo) / 2;
             const int c = __syncthreads_count(key >= at);
             if (c < p.n) {
                 hi = at;
@@ -317,27 +404,55 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
             } else {
                 lo = at;
                 out = false;
-                if (c <= 2 * p.n) break;
+                if (c <= p.n + (p.n + 1) / 2) break;
             }
         }
-        low = lo > 0x007fffffu ? from_ordered_bits(lo) : DISCO_NEG_INF;
-    }
-    float floor = low;
+        return lo > 0x007fffffu ? from_ordered_bits(lo) : DISCO_NEG_INF;
+    };
+    float floor = find_floor(low, 0);
     const int width = deal.merged * CHUNK;
-    auto note_piece = [&](int j) {      // its row and its first token
+    auto note_piece = [&](int k, int v, float z) {      // its row, its first token, its largest logit
         const int at = atomicAdd(&s_pieces, 1);
-        if (at < kBeamPieceList) s_piece[at] = make_int2(item_row(j), item_piece(j) * width);
+        if (at < kBeamPieceList) s_piece[at] = make_int2(k, v), s_piece_top[at] = z;
     };
     auto within = [&](int k, float z) { return z > DISCO_NEG_INF && !((z + s_offset[k]) + (s_err[k] + 0x1p-21f * fabsf(z)) < floor); };
+    auto bound = [&](int k, float z) {
+        const float f = z + s_offset[k];
+        return f < -DISCO_NEG_INF ? f - (s_err[k] + 0x1p-21f * fabsf(z)) : DISCO_NEG_INF;
+    };
 #pragma unroll
     for (int j = 0; j < kBeamItems; ++j)
-        if (item_used(j) && best[j] > DISCO_NEG_INF && !(high[j] < floor)) note_piece(j);
+        if (item_used(j) && best[j] > DISCO_NEG_INF && !(high[j] < floor)) note_piece(item_row(j), item_piece(j) * width, best[j]);
     __syncthreads();
+    const int few = 2 * p.n + 8;      // more than this are worth another search
+    int L = s_pieces, turn = 0;
+    if (L > few && L <= kBeamPieceList) {
+        constexpr int kEach = (kBeamPieceList + THREADS - 1) / THREADS;
+        int2 piece[kEach];
+        float z[kEach], low = DISCO_NEG_INF;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            z[i] = DISCO_NEG_INF;
+            if (i * THREADS + tid >= L) continue;
+            piece[i] = s_piece[i * THREADS + tid];
+            z[i] = s_piece_top[i * THREADS + tid];
+            low = fmaxf(low, bound(piece[i].x, z[i]));
+        }
+        const float next = find_floor(low, 1);
+        __syncthreads();
+        if (tid == 0) s_pieces = 0;
+        floor = fmaxf(floor, next);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (z[i] > DISCO_NEG_INF && within(piece[i].x, z[i])) note_piece(piece[i].x, piece[i].y, z[i]);
+        __syncthreads();
+        L = s_pieces;
+    }
     auto score_of = [&](int k, float z) { return ordered_bits64(static_cast<double>(s_score[k]) + (static_cast<double>(z) - s_lse[k])); };
     auto finish_lse = [&] {
         for (int k = tid; k < p.K; k += THREADS) s_lse[k] = static_cast<double>(s_top[k]) + log(s_lse[k]);
     };
-    int L = s_pieces, turn = 0;
     const bool crowded = L > kBeamPieceList;
     if (crowded) {
         finish_lse();
@@ -358,7 +473,7 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kBeamItems; ++j)
-            if (key[j] > t || (key[j] == t && piece_place(j) <= limit)) note_piece(j);
+            if (key[j] > t || (key[j] == t && piece_place(j) <= limit)) note_piece(item_row(j), item_piece(j) * width, best[j]);
         // (more pieces than the list holds, so n at least have been found)
         floor = __double2float_rd(from_ordered_bits64(t));
         __syncthreads();
@@ -375,10 +490,10 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         return v < p.V;
     };
     auto logit = [&](int k, int v) { return load_logit(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld + v); };
-    auto place_of = [&](int k, int v) { return (long long)k << 32 | v; };
-    auto take = [&](unsigned long long x, long long place) {
+    auto place_of = [&](int k, int v) { return (unsigned long long)k << 32 | (unsigned int)v; };
+    auto take = [&](unsigned long long x, unsigned long long place) {
         const int at = atomicAdd(&s_count, 1);
-        if (at < kBeamList) s_key[at] = x, s_place[at] = place;
+        if (at < kBeamList) s_cand[at] = make_ulonglong2(x, place);
     };
     constexpr int kAhead = 4;
     bool first = !crowded;
@@ -399,10 +514,30 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     if (first) finish_lse();
     if (tid < p.K && s_state[tid] == 2) take(0ull, place_of(tid, p.eos));
     __syncthreads();
-    if (s_count <= kBeamList) {
-        for (int i = tid; i < s_count; i += THREADS) {
-            const int k = static_cast<int>(s_place[i] >> 32);
-            s_key[i] = s_state[k] == 2 ? ordered_bits64(s_score[k]) : score_of(k, __uint_as_float(static_cast<uint32_t>(s_key[i])));
+    int N = s_count;
+    if (N <= kBeamList) {
+        constexpr int kEach = (kBeamList + THREADS - 1) / THREADS;
+        ulonglong2 cand[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) cand[i] = i * THREADS + tid < N ? s_cand[i * THREADS + tid] : make_ulonglong2(0ull, ~0ull);
+        auto row_of = [](const ulonglong2& c) { return static_cast<int>(c.y >> 32); };
+        auto logit_of = [](const ulonglong2& c) { return __uint_as_float(static_cast<uint32_t>(c.x)); };
+        if (N > few) {
+            float low = DISCO_NEG_INF;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (cand[i].y != ~0ull && s_state[row_of(cand[i])] == 1) low = fmaxf(low, bound(row_of(cand[i]), logit_of(cand[i])));
+            floor = fmaxf(floor, find_floor(low, 2));
+        }
+        __syncthreads();
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (cand[i].y == ~0ull) continue;
+            const int k = row_of(cand[i]);
+            if (s_state[k] == 2) take(ordered_bits64(s_score[k]), cand[i].y);
+            else if (within(k, logit_of(cand[i]))) take(score_of(k, logit_of(cand[i])), cand[i].y);
         }
     } else {      // many equal logits
         auto each = [&](auto f) {
@@ -410,9 +545,9 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
                 int k, v;
                 if (!locate(i, k, v)) continue;
                 const float z = logit(k, v);
-                if (z > DISCO_NEG_INF && within(k, z)) f(score_of(k, z), place_of(k, v));
+                if (z > DISCO_NEG_INF && within(k, z)) f(score_of(k, z), static_cast<long long>(place_of(k, v)));
             }
-            if (tid < p.K && s_state[tid] == 2) f(ordered_bits64(s_score[tid]), place_of(tid, p.eos));
+            if (tid < p.K && s_state[tid] == 2) f(ordered_bits64(s_score[tid]), static_cast<long long>(place_of(tid, p.eos)));
         };
         auto values_reach = [&](unsigned long long u, long long limit) {
             int c = 0;
@@ -432,17 +567,19 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     __syncthreads();
 
     // ---- 4 ----
-    const int N = s_count;
+    N = s_count;
     const long long out = (long long)b * p.n;
     for (int i = tid; i < N; i += THREADS) {
-        const unsigned long long x = s_key[i];
-        const long long place = s_place[i];
+        const ulonglong2 c = s_cand[i];
         int rank = 0;
 #pragma unroll 4
-        for (int j = 0; j < N; ++j) rank += s_key[j] > x || (s_key[j] == x && s_place[j] < place);
+        for (int j = 0; j < N; ++j) {       // (no branches: with them a candidate costs 140 cycles)
+            const ulonglong2 o = s_cand[j];
+            rank += static_cast<int>(o.x > c.x) | (static_cast<int>(o.x == c.x) & static_cast<int>(o.y < c.y));
+        }
         if (rank < p.n) {       // (what is read of the beams has been read: the outputs may take the inputs' place)
-            const int parent = static_cast<int>(place >> 32), token = static_cast<int>(place & 0xffffffffll);
-            p.score_out[out + rank] = static_cast<float>(from_ordered_bits64(x));
+            const int parent = static_cast<int>(c.y >> 32), token = static_cast<int>(c.y & 0xffffffffull);
+            p.score_out[out + rank] = static_cast<float>(from_ordered_bits64(c.x));
             p.parent[out + rank] = parent;
             p.token[out + rank] = token;
             if (p.finished_out) p.finished_out[out + rank] = token == p.eos || s_state[parent] == 2;

@@ -168,8 +168,12 @@ BeamParams beam_params(const disco_ctx* c, const void* z, long long ld, int chun
     p.eos = eos;
     p.score = score;
     p.finished = finished;
-    p.stats = c->beam_stats;
     p.chunks = (c->V + chunk - 1) / chunk;
+    p.segs = (p.chunks + kBeamWarpChunks - 1) / kBeamWarpChunks;
+    // (both fit where a pair for each kI8Chunk logits does)
+    p.pairs = c->beam_stats;
+    p.sums = c->beam_stats;
+    p.tops = reinterpret_cast<float*>(c->beam_stats + (size_t)B * K * p.segs);
     p.score_out = score_out;
     p.parent = parent;
     p.token = token;
@@ -179,7 +183,7 @@ BeamParams beam_params(const disco_ctx* c, const void* z, long long ld, int chun
 
 template <typename T, int CHUNK>
 int launch_beam_select(disco_ctx* c, BeamParams p, cudaStream_t st) {
-    const int warps = BeamDeal::warps(p.K, p.chunks);
+    const int warps = BeamDeal::warps(p.K, p.chunks, p.n);
     p.deal = BeamDeal::make(p.K, p.chunks, warps);
     auto kern = warps == 8 ? beam_select_kernel<T, CHUNK, 256> : warps == 16 ? beam_select_kernel<T, CHUNK, 512> : beam_select_kernel<T, CHUNK, 1024>;
     const cudaError_t e = launch_after(c, kern, dim3((unsigned)p.B), dim3((unsigned)(32 * warps)), 0, st, p);
@@ -189,7 +193,7 @@ int launch_beam_select(disco_ctx* c, BeamParams p, cudaStream_t st) {
 
 template <typename T>
 int select_beams(disco_ctx* c, const BeamParams& p, cudaStream_t st) {
-    const long long warps = (long long)p.B * p.K * ((p.chunks + kBeamWarpChunks - 1) / kBeamWarpChunks);
+    const long long warps = (long long)p.B * p.K * p.segs;
     const long long ctas = (warps + kBeamStatWarps - 1) / kBeamStatWarps;
     if (ctas > 0x7fffffffll) return DISCO_ERR_UNSUPPORTED_SHAPE;
     const cudaError_t e = launch_after(c, beam_stats_kernel<T>, dim3((unsigned)ctas), dim3(kBeamStatWarps * 32), 0, st, p);

@@ -301,6 +301,21 @@ __device__ __forceinline__ void store_logit(float* p, float z) { *p = z; }
 __device__ __forceinline__ void store_logit(__nv_bfloat16* p, float z) { *p = __float2bfloat16_rn(z); }
 __device__ __forceinline__ void store_logit(__half* p, float z) { *p = __float2half_rn(z); }
 
+// exp(x - m) for many x and one m: 2^(c x - M) with c = log2 e and M = c m rounded, a single rounding; what M lost to its own rounding is
+// made good once, in the sum.  (Two operations instead of three where they are what bounds the kernel.)  |m| < 2^100.
+struct ExpFrom {
+    static constexpr float c = 1.4426950408889634f;
+    float M;
+    __device__ __forceinline__ explicit ExpFrom(float m) : M(c * m) {}
+    __device__ __forceinline__ float operator()(float x) const {
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(x, c, -M)));
+        return e;
+    }
+    __device__ __forceinline__ float sum(float s, float m) const { return s * exp2f(fmaf(-m, c, M)); }      // (M - c m, exactly)
+    static __device__ __forceinline__ bool serves(float m) { return fabsf(m) < 0x1p100f; }
+};
+
 // Soft-max statistics of 32 vocabulary rows' logits, one per lane, of 16 hidden rows: the largest of each hidden row's (NaN if there is
 // one that is not a number) and the sum of exp(z - largest).  By way of a corner turn in shared memory: two lanes to a hidden row, 16
 // logits each.  // turn: 16 x kI8TurnStride floats of the warp.  Lane i and lane i + 16 return those of hidden row i.
@@ -324,12 +339,18 @@ __device__ __forceinline__ float2 warp_chunk_stats(const float* z, bool in, int 
 #pragma unroll
     for (int j = 1; j < 16; ++j) m = max_nan(m, x[j]);
     m = max_nan(m, __shfl_xor_sync(kFullMask, m, 16));
-    float e[2] = {0.f, 0.f};
+    float e[4] = {0.f, 0.f, 0.f, 0.f};
+    if (__all_sync(kFullMask, ExpFrom::serves(m))) {
+        const ExpFrom from(m);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) e[j & 1] += __expf(x[j] - m);
-    float sum = e[0] + e[1];
-    sum += __shfl_xor_sync(kFullMask, sum, 16);
-    return make_float2(m, sum);      // (NaN where the largest is not finite: nothing is done with it there)
+        for (int j = 0; j < 16; ++j) e[j & 3] += from(x[j]);
+        e[0] = from.sum((e[0] + e[1]) + (e[2] + e[3]), m);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) e[j & 3] += __expf(x[j] - m);
+        e[0] = (e[0] + e[1]) + (e[2] + e[3]);
+    }
+    return make_float2(m, e[0] + __shfl_xor_sync(kFullMask, e[0], 16));      // (NaN where the largest is not finite: nothing is done with it there)
 }
 
 // 32 lanes x 16 consecutive 32-bit columns -> 16 registers per thread

@@ -15,11 +15,12 @@ pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 I32, U8 = torch.int32, torch.uint8
 
-# How far the logarithm of a row's sum of exponentials may be off.  A term e^-t comes from an exponential good to 2^-22 of a product t * log2 e
-# that is rounded to fp32, |t| 2^-24 * 1.5; weighted with the term itself that is at most 2^-22 + 0.37 * 1.5 * 2^-24 < 2^-21.7.  The sums of a
-# chunk's terms are taken in units of 2^-24 (32 lanes, half a unit each: 2^-20 of a sum that is at least 1) or finer; the sum of up to four terms
-# in a lane and the rounding of the chunk's sum, and its weight e^-t, another 2^-21.  In all below 2^-19.
-LSE_TOL = 2.0 ** -19
+# How far the logarithm of a row's sum of exponentials may be off, which is how far the sum may be off relatively.  A term 2^-t comes from an
+# exponential good to 2^-22, of a t rounded to fp32 and formed with a rounded log2 e: weighted with the term itself, t 2^-t <= 0.53, below
+# 2^-21.7 in all.  Ten additions in fp32 bring the terms of a warp together (2^-20.7), a factor makes good what the largest logit's product
+# lost (2^-23); the sums of a lane's chunks, up to eight of them, meet with weights that are such terms again (2^-21.7 + 2^-21), and so do
+# those of a row's warps, in 64 bits (2^-21.7): 2^-18.9.  Rows that are dealt out in several rounds repeat a weight or two.
+LSE_TOL = 2.0 ** -18
 
 
 def score_tol(score):
