@@ -529,15 +529,21 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
                 if (cand[i].y != ~0ull && s_state[row_of(cand[i])] == 1) low = fmaxf(low, bound(row_of(cand[i]), logit_of(cand[i])));
             floor = fmaxf(floor, find_floor(low, 2));
         }
-        __syncthreads();
-        if (tid == 0) s_count = 0;
-        __syncthreads();
+        const bool again = N > few;
+        if (again) {
+            __syncthreads();
+            if (tid == 0) s_count = 0;
+            __syncthreads();
+        }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             if (cand[i].y == ~0ull) continue;
             const int k = row_of(cand[i]);
-            if (s_state[k] == 2) take(ordered_bits64(s_score[k]), cand[i].y);
-            else if (within(k, logit_of(cand[i]))) take(score_of(k, logit_of(cand[i])), cand[i].y);
+            const bool ended = s_state[k] == 2;
+            if (again && !ended && !within(k, logit_of(cand[i]))) continue;
+            const unsigned long long x = ended ? ordered_bits64(s_score[k]) : score_of(k, logit_of(cand[i]));
+            if (again) take(x, cand[i].y);
+            else s_cand[i * THREADS + tid].x = x;
         }
     } else {      // many equal logits
         auto each = [&](auto f) {

@@ -130,7 +130,7 @@ template <typename Out, bool STATS>
 int project(disco_ctx* c, const int8_t* W_q, long long ldw, const float* w_scale, const void* H, int h_type, long long ldh, int d, int R, void* y,
             long long ldy, cudaStream_t st) {
     const Int8Tiling t = Int8Tiling::choose(R, c->V, d, c->sm_count);
-    if (Int8Ring::few(R, d)) {
+    if (Int8Ring::few(R, c->V, d)) {
         switch (h_type) {
             case DISCO_F32: return launch_int8_head<Out, float, STATS, false>(c, t, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);
             case DISCO_BF16: return launch_int8_head<Out, __nv_bfloat16, STATS, false>(c, t, W_q, ldw, w_scale, H, ldh, d, R, y, ldy, st);

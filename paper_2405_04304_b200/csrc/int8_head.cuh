@@ -30,10 +30,7 @@ constexpr int kQuantMaxWidth = 16384;
 //     of x, at most 254 * 2^11 of them, so they differ by 2^-19 of their size or not at all.
 //   * fp32: the same in 64 bits (127 x is exact there, and 254 * 2^24 is well below 2^53).
 template <typename T>
-__device__ __forceinline__ int quantize_one(float x, float top, float inv) {
-    const float p = x * inv;
-    const float r = rintf(p);
-    if (fabsf(p - r) < 0.4995f) return static_cast<int>(r);
+__device__ __noinline__ int quantize_exactly(float x, float top) {
     if constexpr (sizeof(T) == 2) return __float2int_rn(__fdiv_rn(x * 0.9921875f, top) * 128.f);
     else return __double2int_rn(__ddiv_rn(127.0 * static_cast<double>(x), static_cast<double>(top)));
 }
@@ -50,14 +47,29 @@ struct RowScale {
         top *= shift;
         inv = finite && top > 0.f ? 127.f / top : 0.f;
     }
-    // Eight numbers in 8 bits each.
+    // Eight numbers in 8 bits each.  (The rare quotient is a call: in line, 64 times over, it made the kernels' code several times as long, and
+    // code that runs once per launch comes from L2.)
     template <typename T>
     __device__ __forceinline__ uint2 round(const float (&f)[8]) const {
-        uint32_t w[2] = {0u, 0u};
-        if (inv > 0.f) {
+        if (!(inv > 0.f)) return make_uint2(0u, 0u);
+        int r[8];
+        bool close = false;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j >> 2] |= (static_cast<uint32_t>(quantize_one<T>(f[j] * shift, top, inv)) & 0xffu) << (8 * (j & 3));
+        for (int j = 0; j < 8; ++j) {
+            const float p = f[j] * shift * inv;
+            r[j] = __float2int_rn(p);
+            close = close || fabsf(p - static_cast<float>(r[j])) >= 0.4995f;
         }
+        if (close) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float p = f[j] * shift * inv;
+                if (fabsf(p - static_cast<float>(r[j])) >= 0.4995f) r[j] = quantize_exactly<T>(f[j] * shift, top);
+            }
+        }
+        uint32_t w[2] = {0u, 0u};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j >> 2] |= (static_cast<uint32_t>(r[j]) & 0xffu) << (8 * (j & 3));
         return make_uint2(w[0], w[1]);
     }
 };
@@ -160,7 +172,7 @@ constexpr int kI8BK = 128;                // k elements per stage (one 128-byte 
 constexpr int kI8MaxStages = 24;
 constexpr int kI8EpiWarps = 16;
 constexpr int kI8Threads = (2 + kI8EpiWarps) * 32;
-constexpr int kI8FewChunks = 8;           // of eight numbers, that a lane holds of a row which the kernel rounds itself
+constexpr int kI8FewChunks = 4;           // of eight numbers, that a lane holds of a row which the kernel rounds itself
 constexpr int kI8FixedSmem = 1024 /*align*/ + 512 /*barriers*/ + 2 * 256 * 4 /*scales of two tiles' hidden rows*/;
 
 __host__ __device__ inline int round_up(int x, int to) { return (x + to - 1) / to * to; }
@@ -246,12 +258,14 @@ struct Int8Ring {
         if (stages >= 2) r.stages = stages, r.bytes = size(r, t, stages);
         return r;
     }
-    // Hidden rows that the kernel rounds itself, in every CTA (its epilogue's warps have nothing else to do meanwhile): where they are few
-    // enough for a lane to hold its part of them, and to lie in shared memory beside the stages.  (A pass of 1 row of a 32000 x 768 head
-    // 9.6 -> 7.4 us; with rows that are read twice, 11 of 32000 x 5120 30 -> 42.)
-    __host__ __device__ static bool few(int R, int d) {
-        if (R > kI8EpiWarps || (d + kI8BK - 1) / kI8BK * 16 * kI8BK > 96 * 1024) return false;
-        return d <= kI8EpiWarps / R * 256 * kI8FewChunks;
+    // Hidden rows that the kernel rounds itself, in every CTA (its epilogue's warps have nothing else to do meanwhile), rather than a kernel
+    // before it: where a lane can hold its part of them, and there are few enough that their loads do not wait behind the head's.  (us a pass,
+    // a kernel before -> in the kernel: 1 / 4 / 16 rows of 32000 x 768 9.4 / 9.4 / 9.4 -> 7.8 / 7.0 / 8.3; 1 / 4 / 8 / 16 of 32000 x 2048 15.4 /
+    // 15.7 / 16.0 / 16.6 -> 14.6 / 15.3 / 17.1 / 19.2; 1 / 4 of 32000 x 5120 29.9 / 30.2 -> 30.1 / 31.8; 1 / 8 of 49152 x 1024 12.0 / 12.3 ->
+    // 11.7 / 12.5.)
+    __host__ __device__ static bool few(int R, int V, int d) {
+        if (R > kI8EpiWarps || d > 2048 || d > kI8EpiWarps / R * 256 * kI8FewChunks) return false;
+        return R * d <= ((long long)V * d <= 32ll << 20 ? 16384 : 8192);
     }
 };
 

@@ -26,13 +26,13 @@ int main() {
                     // accumulators of all buffers, as columns of tensor memory; reads of 32 columns end inside theirs
                     ok = ok && t.bufs * t.blocks * t.cols <= 512 && t.cols >= t.N && t.cols % 32 == 0;
                   for (int d : {8, 136, 768, 5120, 6144, 16384}) {
-                    const bool few = !pairs && Int8Ring::few(R, d);
+                    const bool few = !pairs && Int8Ring::few(R, V, d);
                     const Int8Ring r = Int8Ring::make(t, d, 227 * 1024 - kI8TurnBytes, few);
                     ok = ok && r.stages >= 2 && r.stages <= kI8MaxStages && kI8FixedSmem + kI8TurnBytes + r.bytes + r.resident <= 227 * 1024;
                     ok = ok && r.w_bytes % 1024 == 0 && r.x_bytes % 1024 == 0 && r.w_bytes >= t.w_box * kI8BK;
                     // the hidden-row boxes of a tile are what its MMA takes, or all there are
                     ok = ok && (pairs ? 2 * t.x_box == t.N : t.x_box == t.N || (t.x_box >= R && t.x_box % 8 == 0));
-                    if (few) { ok = ok && R <= kI8EpiWarps && t.MT == 1 && r.resident >= (d + 127) / 128 * 128 * t.N && r.resident % 1024 == 0; }
+                    if (few) { ok = ok && R <= kI8EpiWarps && t.MT == 1 && t.N == 16 && d <= kI8EpiWarps / R * 256 * kI8FewChunks && r.resident >= (d + 127) / 128 * 128 * t.N && r.resident % 1024 == 0; }
                     else ok = ok && r.x_bytes * ctas >= t.N * kI8BK;
                     // what the last stage's MMAs read
                     ok = ok && (r.stages - 1) * r.w_bytes + t.blocks * 128 * kI8BK <= r.bytes && r.stages * (r.w_bytes + r.x_bytes) <= r.bytes;
