@@ -679,6 +679,23 @@ def test_other_calls_of_the_same_context_keep_their_results():
         assert torch.equal(got[4].cpu().long(), want[1]) and torch.equal(got[5].cpu().long(), want[2])
 
 
+def test_projects_on_many_streams_at_once():
+    V, d, R = 9001, 512, 160
+    g = gen(61)
+    Wq, ws = head(V, d, g)
+    H = [randn(g, R, d).bfloat16() for _ in range(6)]
+    want = [logits_of(Wq, ws, h) for h in H]
+    contexts, streams = [context(V, d, rows=R) for _ in H], [torch.cuda.Stream() for _ in H]
+    y = [torch.zeros((R, V), device="cuda") for _ in H]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, st, h, out in zip(contexts, streams, H, y):
+            c.project_int8(Wq, ws, h, out, stream=st)
+    torch.cuda.synchronize()
+    for c, out, w in zip(contexts, y, want):
+        assert torch.equal(out, w) and c.device_status() == 0
+
+
 # ------------------------------------------------------------------------------------------------ what is refused
 def refused(code, call, *args, **kw):
     with pytest.raises(binding.DiscoError) as e:
