@@ -378,6 +378,35 @@ def test_select_large_rows():
     check_select(randn(g, 1, V), beam_scores(g, 1, 1), 3)
 
 
+@pytest.mark.parametrize("K,n,V", [(7, 7, 3000), (8, 8, 9000), (9, 12, 2000), (16, 24, 30000), (17, 17, 2500), (31, 40, 1200), (32, 32, 5000), (33, 33, 900), (40, 80, 4100),
+                                   (63, 20, 2050), (64, 10, 20011), (48, 100, 18500)])
+def test_select_beams_dealt_to_warps(K, n, V):
+    """One, two and more warps to a beam, two beams to a warp, several chunks to a piece."""
+    g = gen(K * 7 + n)
+    z, score = randn(g, 2 * K, V) * 1.5, beam_scores(g, 2, K) * 0.2
+    score[1, K // 2:] = -math.inf
+    check_select(z, score, n)
+
+
+def test_select_scores_of_any_size():
+    """Scores that leave nothing of the logits' differences (equal, then: by place), and logits of any size."""
+    g = gen(17)
+    z = randn(g, 12, 700)
+    score = torch.tensor([[-1e30, -1e30, -3e38], [1e30, 1e30, 0.0], [3e38, -3e38, -3e38], [0.0, -0.0, -1e-40]], device="cuda")
+    z[3] *= 1e30
+    z[8] = 3e38
+    z[8, 100:] = -3e38
+    check_select(z, score, 9)
+
+
+def test_select_logits_on_a_coarse_grid():
+    """bf16 logits with few values: many pieces hold the same best one."""
+    g = gen(18)
+    z = (randn(g, 20, 30000) * 2.0).round().bfloat16()
+    check_select(z, beam_scores(g, 4, 5), 10)
+    check_select(z[:4], beam_scores(g, 1, 4), 128)
+
+
 def test_select_twice_on_one_context_and_captured():
     g = gen(13)
     B, K, V = 3, 4, 2000
