@@ -21,6 +21,7 @@ constexpr int kBeamChunk = 128;          // logits to a chunk of the pass over g
 constexpr int kBeamWarpChunks = 8;       // chunks that a warp takes, so that 32 loads are on their way at once
 constexpr int kBeamStatWarps = 8;
 constexpr int kBeamThreads = 1024;       // of the selection, at most
+constexpr int kBeamCluster = 8;          // CTAs that make the pass over a sequence's logits and select, in one launch
 constexpr int kBeamItems = 8;            // pieces of rows that a thread of it holds
 constexpr int kBeamMaxKept = DISCO_MAX_KEPT;
 constexpr int kBeamMaxBeams = DISCO_MAX_BEAMS;
@@ -50,6 +51,11 @@ struct BeamDeal {
         return 32;
     }
 };
+
+// The pass over the logits and the selection in one launch: where a cluster has a warp for each segment of a sequence's logits, and the
+// clusters fit side by side.  (us a pass, two launches -> one: 1 / 4 / 16 / 64 x 4 beams of 32000 fp32 logits 14.0 / 10.4 / 11.1 / 14.8 -> 8.9 /
+// 9.5 / 10.4 / 15.4; with two segments to a warp and more, 20 x 5 of 40011 bf16 13.6 -> 14.9, 1 x 16 of 49152 fp32 11.3 -> 16.7.)
+__host__ __device__ inline bool beam_joined(int B, int K, int segs) { return B <= 32 && K * segs <= 16 * kBeamCluster; }
 
 struct BeamParams {
     const void* z;               // [B * K, V] logits, rows ld elements apart
@@ -97,16 +103,9 @@ __device__ __forceinline__ bool beam_expands(const BeamParams& p, int row) {
 // at each of the first three; with two reductions over the warp for each chunk the pass over bf16 logits took as long as over twice as many
 // bytes of fp32.)
 template <typename T>
-__global__ void __launch_bounds__(kBeamStatWarps * 32) beam_stats_kernel(const BeamParams p) {
+__device__ __forceinline__ void beam_stats(const BeamParams& p, long long row, int seg, int lane) {
     static_assert(kBeamWarpChunks == 8, "three halvings");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const long long w = (long long)blockIdx.x * kBeamStatWarps + (threadIdx.x >> 5);
-    const long long row = w / p.segs;
-    if (row >= (long long)p.B * p.K) return;
-    if (!beam_expands(p, (int)row)) return;
-    const int seg = (int)(w % p.segs), first = seg * kBeamWarpChunks;
+    const int first = seg * kBeamWarpChunks;
     // a lane's logits of a chunk: two by two neighbours of 16 bits, so that they can be loaded together, every 32nd of 32 bits
     constexpr int kNext = sizeof(T) == 2 ? 2 : 1;
     const int v0 = first * kBeamChunk + lane * kNext;
@@ -168,6 +167,16 @@ __global__ void __launch_bounds__(kBeamStatWarps * 32) beam_stats_kernel(const B
     if (lane == 0) p.sums[row * p.segs + seg] = make_float2(m, serves ? from.sum(s[0], m) : s[0]);      // (no number where the largest is not finite: nothing is done with it)
 }
 
+template <typename T>
+__global__ void __launch_bounds__(kBeamStatWarps * 32) beam_stats_kernel(const BeamParams p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const long long w = (long long)blockIdx.x * kBeamStatWarps + (threadIdx.x >> 5);
+    const long long row = w / p.segs;
+    if (row >= (long long)p.B * p.K || !beam_expands(p, (int)row)) return;
+    beam_stats<T>(p, row, (int)(w % p.segs), threadIdx.x & 31);
+}
+
 // ---------------------------------------------------------------------------------------------
 // the selection
 // ---------------------------------------------------------------------------------------------
@@ -218,7 +227,7 @@ __device__ __forceinline__ void block_cut(Reach reach, unsigned long long lo, un
     }
 }
 
-// A CTA to a sequence.
+// A CTA to a sequence.  JOINED: a cluster of CTAs, which first of all make the pass over the sequence's logits; one of them goes on.
 //   1  each row's soft-max statistics from its chunks'
 //   2  the pieces that may hold the n best: every piece is known by its best score.  The n-th largest of what the threads have at best is
 //      reached by n pieces at least, and by few more
@@ -227,7 +236,7 @@ __device__ __forceinline__ void block_cut(Reach reach, unsigned long long lo, un
 // Up to 4 everything is in fp32 with a bound on its error, from which a piece or a logit is dropped only if it cannot be among the n best:
 // the 64-bit units are too few for a score for every piece (of 32000 logits and 4 beams, 8400 and 4400 cycles for steps 1 and 2 in 64 bits).
 // Where too many are equal for the lists (a call that is full of ties), the cuts are made in 64 bits, by bisection.
-template <typename T, int CHUNK, int THREADS>
+template <typename T, int CHUNK, int THREADS, bool JOINED>
 __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p) {
     constexpr int kWarps = THREADS / 32;
     __shared__ ulonglong2 s_cand[kBeamList];      // (score, place); in step 3 the logit's bits for the score
@@ -243,7 +252,15 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     __shared__ uint32_t s_best[3];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int b = JOINED ? blockIdx.x / kBeamCluster : blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if constexpr (JOINED) {
+        for (int i = (blockIdx.x % kBeamCluster) * kWarps + warp; i < p.K * p.segs; i += kBeamCluster * kWarps) {
+            const int row = b * p.K + i / p.segs;
+            if (beam_expands(p, row)) beam_stats<T>(p, row, i % p.segs, lane);
+        }
+        cluster_sync();
+        if (blockIdx.x % kBeamCluster) return;
+    }
     const BeamDeal deal = p.deal;
     const int warp_row = deal.two ? warp : warp / deal.share, warp_share = deal.two ? 0 : warp - warp_row * deal.share;
     constexpr int kHalf = kBeamItems / 2;

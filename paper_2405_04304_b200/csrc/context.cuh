@@ -112,12 +112,12 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Clusters of two CTAs, and programmatic stream serialization where that is on.
-inline int launch_attributes(const disco_ctx* c, bool pair, cudaLaunchAttribute (&attr)[2]) {
+// Clusters of CTAs (1: none), and programmatic stream serialization where that is on.
+inline int launch_attributes(const disco_ctx* c, int cluster, cudaLaunchAttribute (&attr)[2]) {
     int n = 0;
-    if (pair) {
+    if (cluster > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = 2;
+        attr[n].val.clusterDim.x = (unsigned)cluster;
         attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
         ++n;
     }

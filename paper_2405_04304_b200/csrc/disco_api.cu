@@ -215,7 +215,7 @@ int launch_umma(disco_ctx* c, const void* W, const void* H, int d, int R, const 
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     cfg.attrs = attr;
-    cfg.numAttrs = launch_attributes(c, pair, attr);
+    cfg.numAttrs = launch_attributes(c, pair ? 2 : 1, attr);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tmap_W, tmap_H, p);
     c->launches += 1;
     return cuda_ok(e, "umma_tail_kernel launch") ? DISCO_OK : DISCO_ERR_CUDA;
@@ -349,7 +349,7 @@ int launch_draft_batch(disco_ctx* c, const void* W, const void* H, int d, int R,
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     cfg.attrs = attr;
-    cfg.numAttrs = launch_attributes(c, pair, attr);
+    cfg.numAttrs = launch_attributes(c, pair ? 2 : 1, attr);
     if (layout) *layout = RecordLayout{p.part_rec, 1, kStampedPieces * p.CN, p.CN, p.TPC * p.TR};
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tmap_W, tmap_H, p, f);
     c->launches += 1;

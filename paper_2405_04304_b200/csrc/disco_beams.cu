@@ -119,7 +119,7 @@ int launch_int8_head(disco_ctx* c, const Int8Tiling& t, const int8_t* W_q, long 
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     cfg.attrs = attr;
-    cfg.numAttrs = launch_attributes(c, PAIR, attr);
+    cfg.numAttrs = launch_attributes(c, PAIR ? 2 : 1, attr);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tmap_W, tmap_X, p);
     c->launches += 1;
     return cuda_ok(e, "int8_head_kernel launch") ? DISCO_OK : DISCO_ERR_CUDA;
@@ -181,25 +181,36 @@ BeamParams beam_params(const disco_ctx* c, const void* z, long long ld, int chun
     return p;
 }
 
-template <typename T, int CHUNK>
+template <typename T, int CHUNK, bool JOINED>
 int launch_beam_select(disco_ctx* c, BeamParams p, cudaStream_t st) {
-    const int warps = BeamDeal::warps(p.K, p.chunks, p.n);
+    int warps = BeamDeal::warps(p.K, p.chunks, p.n);
+    if (JOINED && warps == 8 && p.K * p.segs > 8 * kBeamCluster) warps = 16;      // (a warp to each segment)
     p.deal = BeamDeal::make(p.K, p.chunks, warps);
-    auto kern = warps == 8 ? beam_select_kernel<T, CHUNK, 256> : warps == 16 ? beam_select_kernel<T, CHUNK, 512> : beam_select_kernel<T, CHUNK, 1024>;
-    const cudaError_t e = launch_after(c, kern, dim3((unsigned)p.B), dim3((unsigned)(32 * warps)), 0, st, p);
+    auto kern = warps == 8    ? beam_select_kernel<T, CHUNK, 256, JOINED>
+                : warps == 16 ? beam_select_kernel<T, CHUNK, 512, JOINED>
+                              : beam_select_kernel<T, CHUNK, 1024, JOINED>;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)p.B * (JOINED ? kBeamCluster : 1));
+    cfg.blockDim = dim3((unsigned)(32 * warps));
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    cfg.attrs = attr;
+    cfg.numAttrs = launch_attributes(c, JOINED ? kBeamCluster : 1, attr);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
     c->launches += 1;
     return cuda_ok(e, "beam_select_kernel launch") ? DISCO_OK : DISCO_ERR_CUDA;
 }
 
 template <typename T>
 int select_beams(disco_ctx* c, const BeamParams& p, cudaStream_t st) {
+    if (beam_joined(p.B, p.K, p.segs)) return launch_beam_select<T, kBeamChunk, true>(c, p, st);
     const long long warps = (long long)p.B * p.K * p.segs;
     const long long ctas = (warps + kBeamStatWarps - 1) / kBeamStatWarps;
     if (ctas > 0x7fffffffll) return DISCO_ERR_UNSUPPORTED_SHAPE;
     const cudaError_t e = launch_after(c, beam_stats_kernel<T>, dim3((unsigned)ctas), dim3(kBeamStatWarps * 32), 0, st, p);
     c->launches += 1;
     if (!cuda_ok(e, "beam_stats_kernel launch")) return DISCO_ERR_CUDA;
-    return launch_beam_select<T, kBeamChunk>(c, p, st);
+    return launch_beam_select<T, kBeamChunk, false>(c, p, st);
 }
 
 template <typename Word, int N>
@@ -296,7 +307,7 @@ int disco_beam_step_int8(disco_ctx* c, const int8_t* W_q, long long ldw, const f
     rc = project<float, true>(c, W_q, ldw, w_scale, H, h_type, ldh, d, R, work, c->V, st);
     if (rc) return rc;
     const BeamParams p = beam_params(c, work, c->V, kI8Chunk, B, K, n, score, finished, eos, score_out, parent, token, finished_out);
-    return launch_beam_select<float, kI8Chunk>(c, p, st);
+    return launch_beam_select<float, kI8Chunk, false>(c, p, st);
 }
 
 int disco_beam_reorder(disco_ctx* c, const void* const* src, void* const* dst, int tensors, int B, int K, int n, const int32_t* parent,

@@ -56,6 +56,39 @@ int main() {
 """
 
 
+_DEAL = r"""
+#include "beam.cuh"
+#include <cstdio>
+#include <cstring>
+using namespace disco;
+static unsigned char seen[64 * 20000];
+int main() {
+    for (int K = 1; K <= DISCO_MAX_BEAMS; ++K)
+        for (int chunks : {1, 2, 7, 31, 32, 33, 250, 256, 313, 384, 512, 1000, 1251, 1536, 2048, 8594, 19000})
+            for (int n : {1, 10, 11, 24, 25, 128}) {
+                const int warps = BeamDeal::warps(K, chunks, n);
+                const BeamDeal d = BeamDeal::make(K, chunks, warps);
+                bool ok = (warps == 8 || warps == 16 || warps == 32) && (d.two ? K <= 2 * warps : K * d.share <= warps) && d.merged >= 1;
+                ok = ok && (long long)d.pieces * d.merged >= chunks && (long long)(d.pieces - 1) * d.merged < chunks && d.used <= (d.two ? kBeamItems / 2 : kBeamItems);
+                // every piece of every row belongs to one lane's items, by the same arithmetic as the kernel's
+                std::memset(seen, 0, sizeof(seen));
+                for (int w = 0; w < warps; ++w)
+                    for (int lane = 0; lane < 32; ++lane)
+                        for (int j = 0; j < kBeamItems; ++j) {
+                            const int half = kBeamItems / 2, row0 = d.two ? w : w / d.share, share = d.two ? 0 : w - row0 * d.share;
+                            if ((d.two ? j & (half - 1) : j) >= d.used) continue;
+                            const int k = d.two && j >= half ? row0 + 32 : row0, piece = ((d.two ? j & (half - 1) : j) * d.share + share) * 32 + lane;
+                            if (k < K && piece < d.pieces) ++seen[k * 20000 + piece];
+                        }
+                for (int k = 0; k < K; ++k)
+                    for (int i = 0; i < d.pieces; ++i) ok = ok && seen[k * 20000 + i] == 1;
+                if (!ok) return std::printf("K %d chunks %d n %d\n", K, chunks, n), 1;
+            }
+    return beam_joined(1, 4, 32) && !beam_joined(20, 5, 40) && !beam_joined(64, 4, 32) ? 0 : 2;
+}
+"""
+
+
 def _run(tmp_path, source):
     src, exe = tmp_path / "rules.cu", tmp_path / "rules"
     src.write_text(source)
@@ -69,6 +102,10 @@ def _run(tmp_path, source):
 
 def test_int8_tiling_covers_everything_and_stays_in_its_memory(tmp_path):
     _run(tmp_path, _TILING)
+
+
+def test_every_piece_of_every_row_is_dealt_to_one_lane(tmp_path):
+    _run(tmp_path, _DEAL)
 
 
 def test_null_contexts_are_refused():
