@@ -49,23 +49,27 @@ bool encode_int8_2d(const disco_ctx* c, CUtensorMap* map, const void* base, int 
 }
 
 template <typename T>
-int launch_quantize(disco_ctx* c, const QuantParams& p, int rows, cudaStream_t st) {
+int launch_quantize(disco_ctx* c, const QuantParams& p, cudaStream_t st) {
+    // A warp to a row where there are many narrow ones (32000 x 768 / 40011 x 1000 / 32000 x 2048, a CTA to a row -> a warp: 34 / 45 / 52 -> 19 / 28 / 50 us; a few
+    // rows take as long as one, and a warp needs longer for it).
+    const bool narrow = p.rows >= 2048 && p.d <= 2048;
     const int per_thread = (p.d / 8 + kQuantThreads - 1) / kQuantThreads;
-    auto kern = per_thread <= 1   ? quantize_rows_kernel<T, 1>
-                : per_thread <= 2 ? quantize_rows_kernel<T, 2>
-                : per_thread <= 6 ? quantize_rows_kernel<T, 6>
-                                  : quantize_rows_kernel<T, 16>;
-    const cudaError_t e = launch_after(c, kern, dim3((unsigned)rows), dim3(kQuantThreads), 0, st, p);
+    auto kern = narrow            ? (p.d <= 1024 ? quantize_rows_kernel<T, 4, 1> : quantize_rows_kernel<T, 8, 1>)
+                : per_thread <= 1 ? quantize_rows_kernel<T, 1, 4>
+                : per_thread <= 2 ? quantize_rows_kernel<T, 2, 4>
+                : per_thread <= 6 ? quantize_rows_kernel<T, 6, 4>
+                                  : quantize_rows_kernel<T, 16, 4>;
+    const cudaError_t e = launch_after(c, kern, dim3((unsigned)(narrow ? (p.rows + 3) / 4 : p.rows)), dim3(kQuantThreads), 0, st, p);
     c->launches += 1;
     return cuda_ok(e, "quantize_rows_kernel launch") ? DISCO_OK : DISCO_ERR_CUDA;
 }
 
 int quantize(disco_ctx* c, const void* x, int x_type, long long ldx, int rows, int d, int8_t* q, long long ldq, float* scale, cudaStream_t st) {
-    const QuantParams p{x, ldx, d, q, ldq, scale};
+    const QuantParams p{x, ldx, rows, d, q, ldq, scale};
     switch (x_type) {
-        case DISCO_F32: return launch_quantize<float>(c, p, rows, st);
-        case DISCO_BF16: return launch_quantize<__nv_bfloat16>(c, p, rows, st);
-        default: return launch_quantize<__half>(c, p, rows, st);
+        case DISCO_F32: return launch_quantize<float>(c, p, st);
+        case DISCO_BF16: return launch_quantize<__nv_bfloat16>(c, p, st);
+        default: return launch_quantize<__half>(c, p, st);
     }
 }
 

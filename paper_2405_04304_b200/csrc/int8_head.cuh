@@ -47,29 +47,36 @@ struct RowScale {
         top *= shift;
         inv = finite && top > 0.f ? 127.f / top : 0.f;
     }
-    // Eight numbers in 8 bits each.  (The rare quotient is a call: in line, 64 times over, it made the kernels' code several times as long, and
-    // code that runs once per launch comes from L2.)
+    // Eight numbers in 8 bits each: the sum with 1.5 * 2^23 leaves the nearest integer in its low bits.  (The rare quotient is a call: in line,
+    // 64 times over, it made the kernels' code several times as long, and code that runs once per launch comes from L2.)
     template <typename T>
-    __device__ __forceinline__ uint2 round(const float (&f)[8]) const {
+    __device__ __forceinline__ uint2 round(float (&f)[8]) const {
+        constexpr float kWhole = 12582912.f;
         if (!(inv > 0.f)) return make_uint2(0u, 0u);
-        int r[8];
+        if (shift != 1.f) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] *= shift;
+        }
+        float t[8];
         bool close = false;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float p = f[j] * shift * inv;
-            r[j] = __float2int_rn(p);
-            close = close || fabsf(p - static_cast<float>(r[j])) >= 0.4995f;
+            t[j] = fmaf(f[j], inv, kWhole);
+            close = close || fabsf(fmaf(f[j], inv, kWhole - t[j])) >= 0.4995f;
         }
         if (close) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float p = f[j] * shift * inv;
-                if (fabsf(p - static_cast<float>(r[j])) >= 0.4995f) r[j] = quantize_exactly<T>(f[j] * shift, top);
-            }
+            for (int j = 0; j < 8; ++j)
+                if (fabsf(fmaf(f[j], inv, kWhole - t[j])) >= 0.4995f)
+                    t[j] = __uint_as_float(__float_as_uint(kWhole) + static_cast<uint32_t>(quantize_exactly<T>(f[j], top)));
         }
-        uint32_t w[2] = {0u, 0u};
+        uint32_t w[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j >> 2] |= (static_cast<uint32_t>(r[j]) & 0xffu) << (8 * (j & 3));
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t a = __byte_perm(__float_as_uint(t[4 * h]), __float_as_uint(t[4 * h + 1]), 0x0040);
+            const uint32_t b = __byte_perm(__float_as_uint(t[4 * h + 2]), __float_as_uint(t[4 * h + 3]), 0x0040);
+            w[h] = __byte_perm(a, b, 0x5410);
+        }
         return make_uint2(w[0], w[1]);
     }
 };
@@ -114,55 +121,63 @@ struct QuantChunk<float> {
 struct QuantParams {
     const void* x;
     long long ldx;    // elements
-    int d;            // a multiple of 8
+    int rows, d;      // d: a multiple of 8
     int8_t* q;
     long long ldq;    // a multiple of 16; columns d .. round_up(d, 16) - 1 are written as zeros
     float* scale;
 };
 
-// A CTA to a row; a thread keeps its share of the row (chunks of eight numbers, up to CH of them) in registers between the search
-// for the largest number and the rounding, so that the row is read once.  A row that holds a number that is not finite gets the
-// scale NaN.
-template <typename T, int CH>
+// WPR warps to a row (all four of a CTA, or one for many narrow rows); a thread keeps its share of the row (chunks of eight numbers, up to CH of
+// them) in registers between the search for the largest number and the rounding, so that the row is read once.  A row that holds a number
+// that is not finite gets the scale NaN.
+template <typename T, int CH, int WPR>
 __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const QuantParams p) {
+    constexpr int kRows = kQuantThreads / 32 / WPR;      // of a CTA
     __shared__ uint32_t s_top[kQuantThreads / 32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // (not before the wait: what comes next may read the head ahead of its own, and the head may be what ran before this)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const long long row = blockIdx.x;
+    const long long row = (long long)blockIdx.x * kRows + (threadIdx.x >> 5) / WPR;
+    const bool mine = row < p.rows;
+    const int thread = threadIdx.x % (32 * WPR);
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
-    const int chunks = p.d >> 3;
+    const int chunks = mine ? p.d >> 3 : 0;
     QuantChunk<T> c[CH];
     uint32_t top_bits = 0u;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int at = i * kQuantThreads + threadIdx.x;
-        if (at < chunks) {
-            c[i].load(x + 8 * at);
-            float f[8];
-            c[i].get(f);
+        const int at = i * 32 * WPR + thread;
+        if (at < chunks) c[i].load(x + 8 * at);
+    }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top_bits = max(top_bits, __float_as_uint(f[j]) & 0x7fffffffu);
-        }
+    for (int i = 0; i < CH; ++i) {
+        if (i * 32 * WPR + thread >= chunks) continue;
+        float f[8];
+        c[i].get(f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top_bits = max(top_bits, __float_as_uint(f[j]) & 0x7fffffffu);
     }
     top_bits = __reduce_max_sync(kFullMask, top_bits);
-    if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top_bits;
-    __syncthreads();
+    if constexpr (WPR > 1) {
+        if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top_bits;
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kQuantThreads / 32; ++i) top_bits = max(top_bits, s_top[i]);
+        for (int i = 0; i < kQuantThreads / 32; ++i) top_bits = max(top_bits, s_top[i]);
+    }
+    if (!mine) return;
     const RowScale rs(top_bits);
-    if (threadIdx.x == 0) p.scale[row] = rs.scale;
+    if (thread == 0) p.scale[row] = rs.scale;
     int8_t* q = p.q + row * p.ldq;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int at = i * kQuantThreads + threadIdx.x;
+        const int at = i * 32 * WPR + thread;
         if (at < chunks) {
             float f[8];
             c[i].get(f);
             *reinterpret_cast<uint2*>(q + 8 * at) = rs.template round<T>(f);
         }
     }
-    if ((p.d & 15) && threadIdx.x == 0) *reinterpret_cast<uint2*>(q + p.d) = make_uint2(0u, 0u);
+    if ((p.d & 15) && thread == 0) *reinterpret_cast<uint2*>(q + p.d) = make_uint2(0u, 0u);
 }
 
 // ---------------------------------------------------------------------------------------------
