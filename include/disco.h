@@ -370,7 +370,8 @@ int disco_iteration_host(disco_ctx* ctx, const void* W_D /*device*/, size_t w_st
  * The paper has no counterpart.  A decoder is bound by reading its LM head, and an 8-bit head is half as long; beams are the other
  * use that a draft model's logits are put to.  The calls below need the context's device to be the current one (otherwise
  * DISCO_ERR_INVALID_ARG), take at most max(max_batch, max_rows) rows (DISCO_ERR_WORKSPACE), and read nothing ahead of the
- * work before them in the stream: a head may be quantised right before it is used.
+ * work before them in the stream: a head may be quantised right before it is used.  score, score_out, parent, token, lens and scales
+ * need the alignment of their type only, finished none.
  */
 
 /*
