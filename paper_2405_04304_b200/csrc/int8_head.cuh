@@ -21,7 +21,6 @@ namespace disco {
 // rows to 8 bits
 // ---------------------------------------------------------------------------------------------
 constexpr int kQuantThreads = 128;
-constexpr int kQuantMaxWidth = 16384;
 
 // 127 x / top to the nearest integer, ties to even, with 0 < top < inf, |x| <= top.  The product with the reciprocal is off by less
 // than 127 * 2^-22; only where it comes nearer to the middle between two integers than that is the quotient itself needed.
@@ -347,7 +346,8 @@ struct ExpFrom {
 
 // Soft-max statistics of 32 vocabulary rows' logits, one per lane, of 16 hidden rows: the largest of each hidden row's (NaN if there is
 // one that is not a number) and the sum of exp(z - largest).  By way of a corner turn in shared memory: two lanes to a hidden row, 16
-// logits each.  // turn: 16 x kI8TurnStride floats of the warp.  Lane i and lane i + 16 return those of hidden row i.
+// logits each.
+// turn: 16 x kI8TurnStride floats of the warp.  Lane i and lane i + 16 return those of hidden row i.
 constexpr int kI8TurnStride = 33;
 constexpr int kI8TurnBytes = kI8EpiWarps * 16 * kI8TurnStride * 4;
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -369,7 +369,7 @@ __device__ __forceinline__ float2 warp_chunk_stats(const float* z, bool in, int 
     for (int j = 1; j < 16; ++j) m = max_nan(m, x[j]);
     m = max_nan(m, __shfl_xor_sync(kFullMask, m, 16));
     float e[4] = {0.f, 0.f, 0.f, 0.f};
-    if (__all_sync(kFullMask, ExpFrom::serves(m))) {
+    if (ExpFrom::serves(m)) {       // (by the hidden row's own logits alone: equal rows give equal sums whatever their neighbours are)
         const ExpFrom from(m);
 #pragma unroll
         for (int j = 0; j < 16; ++j) e[j & 3] += from(x[j]);

@@ -185,6 +185,24 @@ def test_project_many_items_to_a_cta():
     check_project(40011, 768, 390)
 
 
+def test_project_large_heads_and_many_rows():
+    check_project(151936, 64, 5)
+    check_project(1_000_003, 8, 2)
+    check_project(3000, 264, 4100)
+    check_project(200, 16384, 700, BF16, F16)
+
+
+def test_project_lowest_integers():
+    """-128 is no rounded number, but a head may hold it."""
+    V, d, R = 1000, 776, 20
+    ctx = context(V, d, rows=R)
+    Wq, ws = head(V, d, gen(9))
+    Wq[::3, ::2] = -128
+    H, y = randn(gen(10), R, d).half(), torch.zeros((R, V), device="cuda")
+    ctx.project_int8(Wq, ws, H, y)
+    assert torch.equal(y, logits_of(Wq, ws, H))
+
+
 def test_project_largest_sums():
     V, d, R = 300, 16384, 4
     ctx = context(V, d, rows=R)
@@ -477,6 +495,26 @@ def test_step_with_hidden_states_that_are_not_numbers():
     assert want[4] > 4 * LSE_TOL
     assert torch.equal(p.cpu().long(), want[1]) and torch.equal(t.cpu().long(), want[2])
     assert (p[1] == -1).all() and (t[1] == -1).all() and not (p[0] == 1).any()
+
+
+def test_step_with_equal_beams_and_one_that_is_not_a_number():
+    """Beams that are equal stay equal, whatever their neighbours are: the lower one first."""
+    V, d, K = 3000, 128, 40
+    ctx = context(V, d, batch=1, rows=K)
+    g = gen(23)
+    Wq, ws = head(V, d, g)
+    ws *= 5.0
+    H, score = randn(g, K, d).bfloat16(), beam_scores(g, 1, K)
+    H[17], H[39] = H[0], H[0]
+    score[0, 17] = score[0, 39] = score[0, 0]
+    H[1, 3], H[35, 0] = math.nan, math.inf
+    n = 24
+    s, p, t = torch.zeros((1, n), device="cuda"), torch.zeros((1, n), dtype=I32, device="cuda"), torch.zeros((1, n), dtype=I32, device="cuda")
+    ctx.beam_step_int8(Wq, ws, H, score, s, p, t, torch.empty((K, V), device="cuda"))
+    want = best_of(logits_of(Wq, ws, H), score, n)
+    assert want[4] > 4 * LSE_TOL
+    assert torch.equal(p.cpu().long(), want[1]) and torch.equal(t.cpu().long(), want[2])
+    assert p[0, :3].tolist() == [0, 17, 39]
 
 
 # ------------------------------------------------------------------------------------------------ states
