@@ -217,18 +217,31 @@ def test_project_largest_sums():
     assert float(y[0, 0]) == float(torch.tensor(127.0 * 127 * d) * (torch.tensor(1.0) / torch.tensor(127.0)) * 0.5)
 
 
-def test_project_rows_that_are_not_finite_or_zero():
-    V, d = 500, 64
-    ctx = context(V, d, rows=40)
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("R,d", [(9, 64), (40, 64), (16, 1000)])
+def test_project_rows_of_any_size(R, d, dtype):
+    """Zeros, the smallest and the largest numbers, borders between integers, what is not finite; rows rounded before and in the kernel."""
+    V = 500
+    ctx = context(V, d, rows=R)
     Wq, ws = head(V, d, gen(1))
-    H = randn(gen(2), 40, d).bfloat16()
-    H[3, 5], H[17, 0], H[20] = math.nan, math.inf, 0.0
-    y = torch.zeros((40, V), device="cuda")
+    info = torch.finfo(dtype)
+    H = randn(gen(2), R, d).to(dtype)
+    H[3, 5], H[7, 0], H[8, 63] = math.nan, math.inf, -math.inf
+    H[0] = 0
+    H[1] = (randn(gen(3), d) * info.tiny).to(dtype)
+    H[2] = 0
+    H[2, 7] = -info.smallest_normal * info.eps
+    H[4, 1] = info.max
+    H[5] = torch.arange(d, device="cuda").to(dtype) % 254
+    H[5, 0] = 254                                  # 127 x / 254: every odd x is a tie
+    y = torch.zeros((R, V), device="cuda")
     ctx.project_int8(Wq, ws, H, y)
     want = logits_of(Wq, ws, H)
-    assert torch.isnan(y[[3, 17]]).all() and (y[20] == 0).all()
-    keep = [r for r in range(40) if r not in (3, 17)]
-    assert torch.equal(y[keep], want[keep])
+    bad = [3, 7, 8]
+    assert torch.isnan(y[bad]).all() and (y[0] == 0).all()
+    keep = [r for r in range(R) if r not in bad]
+    # (sums times a scale of 2.7e36 pass what fp32 holds: infinities by the definition's order of roundings, equal ones)
+    assert not torch.isnan(want[keep]).any() and torch.equal(y[keep], want[keep])
 
 
 # ------------------------------------------------------------------------------------------------ selection
