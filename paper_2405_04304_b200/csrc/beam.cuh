@@ -236,7 +236,7 @@ __device__ __forceinline__ void block_cut(Reach reach, unsigned long long lo, un
 // Up to 4 everything is in fp32 with a bound on its error, from which a piece or a logit is dropped only if it cannot be among the n best:
 // the 64-bit units are too few for a score for every piece (of 32000 logits and 4 beams, 8400 and 4400 cycles for steps 1 and 2 in 64 bits).
 // Where too many are equal for the lists (a call that is full of ties), the cuts are made in 64 bits, by bisection.
-template <typename T, int CHUNK, int THREADS, bool JOINED>
+template <typename T, int CHUNK, int THREADS, bool TWO, bool JOINED>
 __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p) {
     constexpr int kWarps = THREADS / 32;
     __shared__ ulonglong2 s_cand[kBeamList];      // (score, place); in step 3 the logit's bits for the score
@@ -262,17 +262,19 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         if (blockIdx.x % kBeamCluster) return;
     }
     const BeamDeal deal = p.deal;
-    const int warp_row = deal.two ? warp : warp / deal.share, warp_share = deal.two ? 0 : warp - warp_row * deal.share;
-    constexpr int kHalf = kBeamItems / 2;
-    auto item_row = [&](int j) { return deal.two && j >= kHalf ? warp_row + 32 : warp_row; };
-    auto item_piece = [&](int j) { return ((deal.two ? j & (kHalf - 1) : j) * deal.share + warp_share) * 32 + lane; };
-    auto item_used = [&](int j) { return (deal.two ? j & (kHalf - 1) : j) < deal.used; };
+    const int warp_row = TWO ? warp : warp / deal.share, warp_share = TWO ? 0 : warp - warp_row * deal.share;
+    constexpr int kHalf = kBeamItems / 2, kRows = TWO ? 2 : 1;      // (rows of a warp)
+    auto item_row = [&](int j) { return TWO && j >= kHalf ? warp_row + 32 : warp_row; };
+    auto item_piece = [&](int j) { return ((TWO ? j & (kHalf - 1) : j) * deal.share + warp_share) * 32 + lane; };
+    auto item_used = [&](int j) { return (TWO ? j & (kHalf - 1) : j) < deal.used; };
     auto piece_place = [&](int j) { return item_row(j) * deal.pieces + item_piece(j); };
 
     // ---- 1 ----
-    float best[kBeamItems];
+    float best[kBeamItems], top[kRows];      // the largest logits of this lane's pieces, and of those of a row
     {
-        float m[2] = {DISCO_NEG_INF, DISCO_NEG_INF}, e[2] = {0.f, 0.f};
+        float m[kRows], e[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) m[r] = top[r] = DISCO_NEG_INF, e[r] = 0.f;
         // a row's sums join those of this lane: relative to the larger of the largest logits
         auto join = [&](int r, float top, float sum) {
             if (!(top > DISCO_NEG_INF)) return;       // (NaN: the row's largest logit says so)
@@ -282,16 +284,15 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         };
         if constexpr (CHUNK == kBeamChunk) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
+            for (int r = 0; r < kRows; ++r) {
                 const int k = warp_row + 32 * r;
-                if (k >= p.K || (r == 1 && !deal.two)) continue;
+                if (k >= p.K) continue;
                 for (int i = warp_share * 32 + lane; i < p.segs; i += deal.share * 32) {
                     const float2 x = __ldcg(p.sums + (long long)(b * p.K + k) * p.segs + i);
                     join(r, x.x, x.y);
                 }
             }
         }
-        float top[2] = {DISCO_NEG_INF, DISCO_NEG_INF};
 #pragma unroll
         for (int j = 0; j < kBeamItems; ++j) best[j] = DISCO_NEG_INF;
 #pragma unroll 1
@@ -322,37 +323,33 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
 #pragma unroll
             for (int j = 0; j < kBeamItems; ++j) {
                 if (!item_used(j)) continue;
-                const bool r = deal.two && j >= kHalf;
+                const int r = TWO && j >= kHalf;
                 best[j] = max_nan(best[j], x[j].x);
-                top[0] = max_nan(top[0], r ? DISCO_NEG_INF : x[j].x);
-                top[1] = max_nan(top[1], r ? x[j].x : DISCO_NEG_INF);
+                top[r] = max_nan(top[r], x[j].x);
             }
             if constexpr (CHUNK != kBeamChunk) {
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    if (r == 1 && !deal.two) continue;
-                    const float now = warp_max_nan_f32(top[r]);
+                for (int r = 0; r < kRows; ++r) {
+                            const float now = warp_max_nan_f32(top[r]);
                     if (now > m[r]) e[r] *= __expf(m[r] - now);
                     m[r] = now;
 #pragma unroll
                     for (int j = 0; j < kBeamItems; ++j)
-                        if (item_used(j) && (deal.two && j >= kHalf) == (r == 1) && x[j].x > DISCO_NEG_INF)
+                        if (item_used(j) && (TWO && j >= kHalf) == (r == 1) && x[j].x > DISCO_NEG_INF)
                             e[r] = fmaf(x[j].y, __expf(x[j].x - now), e[r]);
                 }
             }
         }
         if constexpr (CHUNK == kBeamChunk) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                if (r == 1 && !deal.two) continue;
-                const float now = warp_max_nan_f32(max_nan(m[r], top[r]));
+            for (int r = 0; r < kRows; ++r) {
+                    const float now = warp_max_nan_f32(max_nan(m[r], top[r]));
                 e[r] = m[r] > DISCO_NEG_INF ? e[r] * __expf(m[r] - now) : 0.f;
                 m[r] = now;
             }
         }
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            if (r == 1 && !deal.two) continue;
+        for (int r = 0; r < kRows; ++r) {
             double sum = e[r];
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(kFullMask, sum, off);
@@ -361,7 +358,7 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     }
     __syncthreads();
     for (int k = warp; k < p.K; k += kWarps) {       // a warp to a row, a lane to a share
-        const int r = k >> 5, w = deal.two ? k & 31 : k * deal.share + lane;
+        const int r = k >> 5, w = TWO ? k & 31 : k * deal.share + lane;
         const float x = lane < deal.share ? s_max[r][w] : DISCO_NEG_INF;
         const float top = warp_max_nan_f32(x);
         const bool is = top > DISCO_NEG_INF && top < -DISCO_NEG_INF;     // (otherwise the row is no distribution)
@@ -382,25 +379,19 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
 
     // ---- 2 ----
     // (a warp's rows, the second one where it has two)
-    float offset[2], err[2];
-    bool expands[2];
+    float offset[kRows], err[kRows];
+    float low = DISCO_NEG_INF;      // the least that the best of this thread's pieces may score
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < kRows; ++r) {
         const int k = warp_row + 32 * r;
-        expands[r] = (r == 0 || deal.two) && k < p.K && s_state[k] == 1;
-        offset[r] = expands[r] ? s_offset[k] : 0.f;
-        err[r] = expands[r] ? s_err[k] : 0.f;
+        const bool expands = k < p.K && s_state[k] == 1;
+        offset[r] = expands ? s_offset[k] : 0.f;
+        err[r] = expands ? s_err[k] : 0.f;
+        if (!expands) top[r] = DISCO_NEG_INF;       // (nothing of this row counts)
+        const float f = top[r] + offset[r];
+        if (top[r] > DISCO_NEG_INF && f < -DISCO_NEG_INF) low = fmaxf(low, f - (err[r] + 0x1p-21f * fabsf(top[r])));       // (beyond what fp32 holds: no bound)
     }
-    float low = DISCO_NEG_INF, high[kBeamItems];      // the least that the best of this thread's pieces may score, the most that each may
-#pragma unroll
-    for (int j = 0; j < kBeamItems; ++j) {
-        if (!item_used(j)) continue;
-        const int r = deal.two && j >= kHalf;
-        if (!expands[r]) best[j] = DISCO_NEG_INF;
-        const float f = best[j] + offset[r], e = err[r] + 0x1p-21f * fabsf(best[j]);
-        if (best[j] > DISCO_NEG_INF && f < -DISCO_NEG_INF) low = fmaxf(low, f - e);       // (beyond what fp32 holds: no bound)
-        high[j] = f + e;
-    }
+    auto high = [&](int r, float z) { return (z + offset[r]) + (err[r] + 0x1p-21f * fabsf(z)); };      // the most that a logit may score
     // The n-th largest of the threads' bounds, or a little less.  Each step costs a barrier that counts, so the search goes out from the
     // largest one, in strides that grow until n reach it, and only then halves what is left.
     auto find_floor = [&](float low, int use) {
@@ -438,8 +429,13 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         return f < -DISCO_NEG_INF ? f - (s_err[k] + 0x1p-21f * fabsf(z)) : DISCO_NEG_INF;
     };
 #pragma unroll
-    for (int j = 0; j < kBeamItems; ++j)
-        if (item_used(j) && best[j] > DISCO_NEG_INF && !(high[j] < floor)) note_piece(item_row(j), item_piece(j) * width, best[j]);
+    for (int r = 0; r < kRows; ++r) {
+        if (!(top[r] > DISCO_NEG_INF) || high(r, top[r]) < floor) continue;      // (so it is with most threads)
+#pragma unroll
+        for (int j = 0; j < kBeamItems; ++j)
+            if (item_used(j) && (TWO && j >= kHalf) == (r == 1) && best[j] > DISCO_NEG_INF && !(high(r, best[j]) < floor))
+                note_piece(item_row(j), item_piece(j) * width, best[j]);
+    }
     __syncthreads();
     const int few = 2 * p.n + 8;      // more than this are worth another search
     int L = s_pieces, turn = 0;
@@ -476,7 +472,8 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         __syncthreads();
         unsigned long long key[kBeamItems];
 #pragma unroll
-        for (int j = 0; j < kBeamItems; ++j) key[j] = best[j] > DISCO_NEG_INF ? score_of(item_row(j), best[j]) : 0ull;
+        for (int j = 0; j < kBeamItems; ++j)
+            key[j] = top[TWO && j >= kHalf] > DISCO_NEG_INF && best[j] > DISCO_NEG_INF ? score_of(item_row(j), best[j]) : 0ull;
         auto pieces_reach = [&](unsigned long long u, long long limit) {
             int c = 0;
 #pragma unroll

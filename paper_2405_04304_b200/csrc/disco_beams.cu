@@ -190,9 +190,10 @@ int launch_beam_select(disco_ctx* c, BeamParams p, cudaStream_t st) {
     int warps = BeamDeal::warps(p.K, p.chunks, p.n);
     if (JOINED && warps == 8 && p.K * p.segs > 8 * kBeamCluster) warps = 16;      // (a warp to each segment)
     p.deal = BeamDeal::make(p.K, p.chunks, warps);
-    auto kern = warps == 8    ? beam_select_kernel<T, CHUNK, 256, JOINED>
-                : warps == 16 ? beam_select_kernel<T, CHUNK, 512, JOINED>
-                              : beam_select_kernel<T, CHUNK, 1024, JOINED>;
+    auto kern = warps == 8    ? beam_select_kernel<T, CHUNK, 256, false, JOINED>
+                : warps == 16 ? beam_select_kernel<T, CHUNK, 512, false, JOINED>
+                : p.deal.two  ? beam_select_kernel<T, CHUNK, 1024, true, JOINED>
+                              : beam_select_kernel<T, CHUNK, 1024, false, JOINED>;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)p.B * (JOINED ? kBeamCluster : 1));
     cfg.blockDim = dim3((unsigned)(32 * warps));
