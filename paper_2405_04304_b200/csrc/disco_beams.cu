@@ -49,23 +49,37 @@ bool encode_int8_2d(const disco_ctx* c, CUtensorMap* map, const void* base, int 
 }
 
 template <typename T>
-int launch_quantize(disco_ctx* c, const QuantParams& p, cudaStream_t st) {
-    // A warp to a row where there are many narrow ones (32000 x 768 / 40011 x 1000 / 32000 x 2048, a CTA to a row -> a warp: 34 / 45 / 52 -> 19 / 28 / 50 us; a few
-    // rows take as long as one, and a warp needs longer for it).
-    const bool narrow = p.rows >= 2048 && p.d <= 2048;
-    const int per_thread = (p.d / 8 + kQuantThreads - 1) / kQuantThreads;
-    auto kern = narrow            ? (p.d <= 1024 ? quantize_rows_kernel<T, 4, 1> : quantize_rows_kernel<T, 8, 1>)
-                : per_thread <= 1 ? quantize_rows_kernel<T, 1, 4>
-                : per_thread <= 2 ? quantize_rows_kernel<T, 2, 4>
-                : per_thread <= 6 ? quantize_rows_kernel<T, 6, 4>
-                                  : quantize_rows_kernel<T, 16, 4>;
-    const cudaError_t e = launch_after(c, kern, dim3((unsigned)(narrow ? (p.rows + 3) / 4 : p.rows)), dim3(kQuantThreads), 0, st, p);
+int launch_quantize(disco_ctx* c, QuantParams p, cudaStream_t st) {
+    void (*kern)(QuantParams);
+    int threads = kQuantThreads, ctas = p.rows;
+    if (p.rows >= 2048) {
+        // A head: a warp to a narrow row, four to a wide one (32000 x 768 / 40011 x 1000 / 32000 x 5120: 19 / 28 / 105 us; four warps to a narrow
+        // row 34 / 45, sixteen to a wide one 171).
+        if (p.d <= 2048) ctas = (p.rows + 3) / 4;
+        kern = p.d <= 1024   ? quantize_rows_kernel<T, 4, 1>
+               : p.d <= 2048 ? quantize_rows_kernel<T, 8, 1>
+               : p.d <= 6144 ? quantize_rows_kernel<T, 6, 4>
+                             : quantize_rows_kernel<T, 16, 4>;
+    } else {
+        // Hidden rows, which a product waits for: two chunks to a thread at most while the warps of a CTA go round (us a pass of 64 / 128 / 256
+        // rows of a 32000 x 5120 head, four warps -> sixteen: 32.4 / 36.4 / 48.1 -> 31.6 / 34.8 / 45.0).
+        threads = p.d <= 2048 ? 128 : p.d <= 4096 ? 256 : 512;
+        kern = p.d <= 1024   ? quantize_rows_kernel<T, 1, 4>
+               : p.d <= 2048 ? quantize_rows_kernel<T, 2, 4>
+               : p.d <= 4096 ? quantize_rows_kernel<T, 2, 8>
+               : p.d <= 8192 ? quantize_rows_kernel<T, 2, 16>
+                             : quantize_rows_kernel<T, 4, 16>;
+        // Many of them would be read behind the head's first tiles, which the product's CTAs request as soon as they may start (704 rows 108.7 ->
+        // 105.3 us; 11 / 256 rows 30.0 / 45.0 -> 30.3 / 46.4).
+        p.late = p.rows >= 512;
+    }
+    const cudaError_t e = launch_after(c, kern, dim3((unsigned)ctas), dim3((unsigned)threads), 0, st, p);
     c->launches += 1;
     return cuda_ok(e, "quantize_rows_kernel launch") ? DISCO_OK : DISCO_ERR_CUDA;
 }
 
 int quantize(disco_ctx* c, const void* x, int x_type, long long ldx, int rows, int d, int8_t* q, long long ldq, float* scale, cudaStream_t st) {
-    const QuantParams p{x, ldx, rows, d, q, ldq, scale};
+    const QuantParams p{x, ldx, rows, d, q, ldq, scale, 0};
     switch (x_type) {
         case DISCO_F32: return launch_quantize<float>(c, p, st);
         case DISCO_BF16: return launch_quantize<__nv_bfloat16>(c, p, st);

@@ -124,18 +124,19 @@ struct QuantParams {
     int8_t* q;
     long long ldq;    // a multiple of 16; columns d .. round_up(d, 16) - 1 are written as zeros
     float* scale;
+    int late;         // what comes next may start once the rows have been read, not before
 };
 
-// WPR warps to a row (all four of a CTA, or one for many narrow rows); a thread keeps its share of the row (chunks of eight numbers, up to CH of
+// WPR warps to a row (all of a CTA, or one of four for many narrow rows); a thread keeps its share of the row (chunks of eight numbers, up to CH of
 // them) in registers between the search for the largest number and the rounding, so that the row is read once.  A row that holds a number
 // that is not finite gets the scale NaN.
 template <typename T, int CH, int WPR>
-__global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const QuantParams p) {
-    constexpr int kRows = kQuantThreads / 32 / WPR;      // of a CTA
-    __shared__ uint32_t s_top[kQuantThreads / 32];
+__global__ void __launch_bounds__(WPR == 1 ? kQuantThreads : 32 * WPR) quantize_rows_kernel(const QuantParams p) {
+    constexpr int kThreads = WPR == 1 ? kQuantThreads : 32 * WPR, kRows = kThreads / 32 / WPR;      // rows of a CTA
+    __shared__ uint32_t s_top[kThreads / 32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // (not before the wait: what comes next may read the head ahead of its own, and the head may be what ran before this)
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (!p.late) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const long long row = (long long)blockIdx.x * kRows + (threadIdx.x >> 5) / WPR;
     const bool mine = row < p.rows;
     const int thread = threadIdx.x % (32 * WPR);
@@ -157,11 +158,12 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const Quan
         for (int j = 0; j < 8; ++j) top_bits = max(top_bits, __float_as_uint(f[j]) & 0x7fffffffu);
     }
     top_bits = __reduce_max_sync(kFullMask, top_bits);
+    if (p.late) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if constexpr (WPR > 1) {
         if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top_bits;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kQuantThreads / 32; ++i) top_bits = max(top_bits, s_top[i]);
+        for (int i = 0; i < kThreads / 32; ++i) top_bits = max(top_bits, s_top[i]);
     }
     if (!mine) return;
     const RowScale rs(top_bits);

@@ -74,8 +74,8 @@ def check_quantised(ctx, x):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
-@pytest.mark.parametrize("rows,d", [(1, 8), (3, 24), (5, 136), (7, 1000), (2, 1024), (4, 1032), (33, 2048), (2, 6144), (3, 6152), (1, 16384),
-                                    (2047, 136), (2049, 136), (2051, 1000), (3001, 1024), (2050, 1032), (2049, 2048), (2100, 2056)])
+@pytest.mark.parametrize("rows,d", [(1, 8), (3, 24), (5, 136), (7, 1000), (2, 1024), (4, 1032), (33, 2048), (2, 6144), (3, 6152), (1, 16384), (2, 3000), (3, 4096), (2, 4104), (3, 8192), (2, 8200),
+                                    (2047, 136), (2049, 136), (2051, 1000), (3001, 1024), (2050, 1032), (2049, 2048), (2100, 2056), (2048, 6152)])
 def test_quantised_rows(dtype, rows, d):
     ctx = context(64)
     g = gen(rows * 100 + d)
