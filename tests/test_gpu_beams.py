@@ -162,6 +162,11 @@ def test_project_rows(R):
     check_project(5000, 256, R)
 
 
+@pytest.mark.parametrize("V,d,R", [(5000, 2048, 257), (5000, 2104, 577), (9001, 2048, 545), (18001, 2048, 704), (3001, 2504, 961), (18001, 136, 577), (5000, 136, 785)])
+def test_project_with_a_last_tile_of_fewer_rows(V, d, R):
+    check_project(V, d, R)
+
+
 @pytest.mark.parametrize("V", [1, 2, 31, 32, 33, 127, 128, 129, 256, 257, 1000, 4001, 18944, 18945, 37888, 37889, 40011])
 @pytest.mark.parametrize("R", [3, 130])
 def test_project_vocabularies(V, R):
