@@ -436,7 +436,8 @@ int disco_beam_step_int8(disco_ctx* ctx, const int8_t* W_q, long long ldw, const
  *   parent      int32 [B, n]; -1: the child's rows are left as they are; otherwise outside [0, K): the same, and DISCO_ERR_INVALID_ARG
  *               in the device status word
  *   lens        int32 [B] or NULL: positions in use; those behind are left as they are (outside [0, T]: the nearer end)
- * All tensors in place (dst[i] == src[i], n == K; only rows that change are written) or none; other overlaps are refused.
+ * All tensors in place (dst[i] == src[i], n == K; only rows that change are written) or none; other overlaps are refused, those of
+ * one tensor's dst with another's src or dst too (a state listed twice).  Two tensors may have one src.
  */
 int disco_beam_reorder(disco_ctx* ctx, const void* const* src, void* const* dst, int tensors, int B, int K, int n,
                        const int32_t* parent, const int32_t* lens, long long mid, long long T, long long unit_bytes,

@@ -2,6 +2,8 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <memory>
+#include <new>
 
 #include "disco.h"
 #include "context.cuh"
@@ -243,6 +245,30 @@ int launch_reorder(disco_ctx* c, ReorderParams& p, int tensors, cudaStream_t st)
     return cuda_ok(e, "beam_reorder_kernel launch") ? DISCO_OK : DISCO_ERR_CUDA;
 }
 
+// What is written lies apart from all else that is written, and (unless in place) read: a state that is there twice would be reordered
+// twice at once.
+int check_apart(const void* const* src, size_t src_bytes, void* const* dst, size_t dst_bytes, int tensors, bool in_place) {
+    auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+    if (tensors == 1) {
+        const uintptr_t s = at(src[0]), d = at(dst[0]);
+        return !in_place && s < d + dst_bytes && d < s + src_bytes ? DISCO_ERR_INVALID_ARG : DISCO_OK;
+    }
+    const std::unique_ptr<uintptr_t[]> held(new (std::nothrow) uintptr_t[tensors]);
+    uintptr_t *first = held.get(), *last = first + tensors;
+    if (!first) return DISCO_ERR_WORKSPACE;
+    std::transform(dst, dst + tensors, first, at);
+    std::sort(first, last);
+    for (const uintptr_t* d = first; d + 1 < last; ++d)
+        if (d[1] - d[0] < dst_bytes) return DISCO_ERR_INVALID_ARG;
+    for (int i = 0; !in_place && i < tensors; ++i) {
+        const uintptr_t s = at(src[i]);
+        const uintptr_t* d = std::upper_bound(first, last, s);       // the first one behind, and the one before it
+        if (d < last && *d - s < src_bytes) return DISCO_ERR_INVALID_ARG;
+        if (d > first && s - d[-1] < dst_bytes) return DISCO_ERR_INVALID_ARG;
+    }
+    return DISCO_OK;
+}
+
 // Words of `size` bytes; in place a thread holds its words of all rows at once.
 int launch_reorder_words(disco_ctx* c, ReorderParams& p, int size, int tensors, cudaStream_t st) {
     const bool many = p.in_place && p.n > 16;
@@ -342,16 +368,15 @@ int disco_beam_reorder(disco_ctx* c, const void* const* src, void* const* dst, i
         T *= mid;
         mid = 1;
     }
-    int in_place = -1;
+    const bool in_place = src[0] == dst[0];
+    if (in_place && n != K) return DISCO_ERR_INVALID_ARG;
     uintptr_t low = (uintptr_t)(lens ? unit_bytes : T * unit_bytes);
     for (int i = 0; i < tensors; ++i) {
-        if (!src[i] || !dst[i]) return DISCO_ERR_INVALID_ARG;
-        const uintptr_t s = reinterpret_cast<uintptr_t>(src[i]), d = reinterpret_cast<uintptr_t>(dst[i]);
-        if (s == d ? n != K : s < d + dst_bytes && d < s + src_bytes) return DISCO_ERR_INVALID_ARG;
-        if (in_place >= 0 && in_place != (s == d)) return DISCO_ERR_INVALID_ARG;
-        in_place = s == d;
-        low |= s | d;
+        if (!src[i] || !dst[i] || (src[i] == dst[i]) != in_place) return DISCO_ERR_INVALID_ARG;
+        low |= reinterpret_cast<uintptr_t>(src[i]) | reinterpret_cast<uintptr_t>(dst[i]);
     }
+    const int rc = check_apart(src, src_bytes, dst, dst_bytes, tensors, in_place);
+    if (rc) return rc;
     if (!on_its_device(c)) return DISCO_ERR_INVALID_ARG;
     // the widest word that divides everything; in place fewer bytes where a thread has to hold many rows' words
     int size = low & 1 ? 1 : low & 2 ? 2 : low & 4 ? 4 : low & 8 ? 8 : 16;

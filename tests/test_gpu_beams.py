@@ -857,6 +857,31 @@ def test_refusals():
     assert ctx.device_status() == 0 and ctx.launch_count() == 0
 
 
+def test_reorder_refuses_states_that_share_memory():
+    ctx = context(8)
+    parent = torch.tensor([[1, 0], [1, 1]], dtype=I32, device="cuda")
+    buf = torch.arange(400, device="cuda").reshape(100, 4).float()
+    at = [buf[i:i + 4] for i in range(97)]
+    before = buf.clone()
+    INV = binding.ERR_INVALID_ARG
+    refused(INV, ctx.beam_reorder, [at[0], at[0]], [at[0], at[0]], parent)                             # a state twice, in place
+    refused(INV, ctx.beam_reorder, [at[0], at[20], at[3]], [at[0], at[20], at[3]], parent)             # ... or a part of it
+    refused(INV, ctx.beam_reorder, [at[0], at[10]], [at[20], at[20]], parent)                          # one place for two states
+    refused(INV, ctx.beam_reorder, [at[0], at[10]], [at[20], at[23]], parent)
+    refused(INV, ctx.beam_reorder, [at[0], at[10]], [at[10], at[20]], parent)                          # another state's place
+    refused(INV, ctx.beam_reorder, [at[0], at[10]], [at[20], at[3]], parent)
+    refused(INV, ctx.beam_reorder, [at[10], at[3]], [at[20], at[0]], parent)
+    refused(INV, ctx.beam_reorder, [at[0], at[10]], [at[10], at[0]], parent)                           # exchanged
+    assert torch.equal(buf, before) and ctx.launch_count() == 0
+    ctx.beam_reorder([at[0], at[0], at[4]], [at[8], at[12], at[16]], parent)                           # one source for two, neighbours
+    ctx.beam_reorder([at[40], at[44]], [at[40], at[44]], parent)
+    rows = [1, 0, 3, 3]
+    assert torch.equal(buf[8:20], torch.cat([before[0:4][rows], before[0:4][rows], before[4:8][rows]]))
+    assert torch.equal(buf[40:48], torch.cat([before[40:44][rows], before[44:48][rows]]))
+    assert torch.equal(buf[:8], before[:8]) and torch.equal(buf[20:40], before[20:40]) and torch.equal(buf[48:], before[48:])
+    assert ctx.device_status() == 0
+
+
 @pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two GPUs")
 def test_another_current_device_is_refused():
     ctx = context(100)
