@@ -857,6 +857,65 @@ def test_refusals():
     assert ctx.device_status() == 0 and ctx.launch_count() == 0
 
 
+def test_offsets_beyond_32_bits():
+    g = gen(77)
+    far = (1 << 31) + 4096                                   # bytes, a multiple of all sizes
+    buf = torch.zeros(7 << 30, dtype=U8, device="cuda")
+
+    def apart(x, step=far):                                  # the rows of x, `step` bytes apart
+        assert x.shape[0] * step <= buf.numel()
+        return buf.view(x.dtype).as_strided(x.shape, (step // x.element_size(), 1)).copy_(x)
+
+    # rows to 8 bits, to rows that lie apart too
+    x = randn(g, 3, 264).to(BF16)
+    q, scale = torch.zeros((3, 272), dtype=torch.int8, device="cuda"), torch.zeros(3, device="cuda")
+    ctx = context(400, 264, batch=1, rows=24)
+    ctx.quantize_rows(apart(x), q, scale)
+    want_q, want_scale = quantised(x)
+    assert torch.equal(q[:, :264].double(), want_q.double()) and torch.equal(scale, want_scale)
+    q_far = buf[:3 * far].view(torch.int8).view(3, far)      # (rows in 8 bits: contiguous, as wide as they are apart)
+    q_far[:, :300] = 9
+    ctx.quantize_rows(x, q_far, scale)
+    assert torch.equal(q_far[:, :264], q[:, :264]) and (q_far[:, 264:272] == 0).all() and (q_far[:, 272:300] == 9).all()
+    # hidden rows, logits and a head that lie apart
+    Wq, ws = head(400, 264, g)
+    for R in (3, 20):                                        # (rounded by the product's kernel, and before it)
+        H = randn(g, R, 264).to(BF16)
+        want = logits_of(Wq, ws, H)
+        y = torch.zeros((R, 400), device="cuda")
+        step = far if R == 3 else 1 << 28
+        ctx.project_int8(Wq, ws, apart(H, step), y)
+        assert torch.equal(y, want)
+        y_far = apart(torch.zeros_like(y), step)
+        ctx.project_int8(Wq, ws, H, y_far)
+        assert torch.equal(y_far, want)
+        y.zero_()
+        W_far = buf[:400 << 24].view(torch.int8).view(400, 1 << 24)      # 6.7 GB
+        W_far[:, :Wq.shape[1]] = Wq
+        ctx.project_int8(W_far, ws, H, y)
+        assert torch.equal(y, want)
+    # logits that lie apart; one launch, and two
+    for V in (400, 20011):
+        check_select(apart(randn(g, 3, V)), beam_scores(g, 1, 3), 4)
+    # states
+    state = buf[:2 * far].view(2, 2, far // 2)               # [beam, head, position]
+    for beam in range(2):
+        state[beam, 0].fill_(3 + beam)
+        state[beam, 1].fill_(5 + beam)
+    both = torch.tensor([[1, 0]], dtype=I32, device="cuda")
+    ctx.beam_reorder([state], [state], both)
+    for beam in range(2):
+        assert (state[beam, 0] == 4 - beam).all() and (state[beam, 1] == 6 - beam).all()
+    parent, child = buf[:far].view(1, far), buf[far:3 * far].view(2, far)
+    used = (1 << 31) - 1
+    parent.copy_(torch.arange(251, dtype=U8, device="cuda").repeat(far // 251 + 1)[:far])
+    child.fill_(253)
+    ctx.beam_reorder([parent], [child], torch.zeros((1, 2), dtype=I32, device="cuda"), lens=torch.full((1,), used, dtype=I32, device="cuda"))
+    for row in child:
+        assert torch.equal(row[:used], parent[0, :used]) and (row[used:] == 253).all()
+    assert ctx.device_status() == 0
+
+
 def test_reorder_refuses_states_that_share_memory():
     ctx = context(8)
     parent = torch.tensor([[1, 0], [1, 1]], dtype=I32, device="cuda")
