@@ -333,7 +333,8 @@ __device__ __forceinline__ void store_logit(__nv_bfloat16* p, float z) { *p = __
 __device__ __forceinline__ void store_logit(__half* p, float z) { *p = __float2half_rn(z); }
 
 // exp(x - m) for many x and one m: 2^(c x - M) with c = log2 e and M = c m rounded, a single rounding; what M lost to its own rounding is
-// made good once, in the sum.  (Two operations instead of three where they are what bounds the kernel.)  |m| < 2^100.
+// made good once, in the sum.  (Two operations instead of three where they are what bounds the kernel.)  |m| < 2^24: M is then off by 1 at
+// most, and the terms by a factor of 2.  (The loss grows with m: at 2^31 the terms would pass what fp32 holds.)
 struct ExpFrom {
     static constexpr float c = 1.4426950408889634f;
     float M;
@@ -344,7 +345,7 @@ struct ExpFrom {
         return e;
     }
     __device__ __forceinline__ float sum(float s, float m) const { return s * exp2f(fmaf(-m, c, M)); }      // (M - c m, exactly)
-    static __device__ __forceinline__ bool serves(float m) { return fabsf(m) < 0x1p100f; }
+    static __device__ __forceinline__ bool serves(float m) { return fabsf(m) < 0x1p24f; }
 };
 
 // Soft-max statistics of 32 vocabulary rows' logits, one per lane, of 16 hidden rows: the largest of each hidden row's (NaN if there is

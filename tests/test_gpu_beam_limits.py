@@ -1,0 +1,75 @@
+"""Selections at the edges of what the arithmetic holds: masks of any size, and logits and scores as large as fp32 has them."""
+import math
+
+import pytest
+import torch
+
+import test_gpu_beams as beams
+from test_gpu_beams import BF16, F16, F32, I32, beam_scores, check_select, gen, head, logits_of, randn
+
+pytestmark = pytest.mark.gpu
+
+MASKS = [-1e5, -1.6e7, -1.7e7, -1e9, -1e10, -1e12, -1e20, -1e30]
+
+
+# ------------------------------------------------------------------------------------------------ masks and large logits
+def masked(g, rows, V, mask, z_type):
+    """Logits of which some tokens are not allowed: whole segments of 1024, parts of them, all but one, whole chunks of 32 and of 128."""
+    z = randn(g, rows, V)
+    z[0, 1024:2048] = mask
+    z[1, :2048] = mask
+    z[2, 1000:] = mask
+    z[3, 1:] = mask
+    z[4, 32:64] = mask
+    z[5, 128:256] = mask
+    z[6, ::2] = mask
+    z[7] = mask + 0.0 * z[7]                        # nothing allowed: every token as good as the others
+    return z.to(z_type)
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("z_type", [F32, BF16])
+@pytest.mark.parametrize("B,V", [(2, 5000), (40, 2500)])          # one launch, and two
+def test_select_masks_of_any_size(mask, z_type, B, V):
+    g = gen(B + V)
+    z = torch.cat([masked(g, 8, V, mask, z_type) for _ in range(B // 2)])
+    check_select(z, beam_scores(g, B, 4), 6)
+
+
+@pytest.mark.parametrize("size", [1.6e7, 1.7e7, 1e9, 1e10, 1e12, 1e20, 1e30])
+@pytest.mark.parametrize("z_type", [F32, BF16])
+def test_select_logits_of_any_size(size, z_type):
+    """Rows whose largest logit is far from 0, on either side."""
+    g = gen(3)
+    z = randn(g, 8, 3000)
+    z[0] += size
+    z[1] -= size
+    z[2, 7] = size
+    z[3, 1500] = size
+    z[4, 100:1200] -= size
+    z[5] *= size
+    check_select(z.to(z_type), beam_scores(g, 2, 4), 5)
+
+
+@pytest.mark.parametrize("size", [1e8, 1e10, 1e12, 1e20, 1e30])
+def test_step_logits_of_any_size(size):
+    """Vocabulary rows whose scale makes logits of any size, by whole chunks and one by one, on either side of 0."""
+    V, d, B, K, n = 3000, 128, 2, 3, 5
+    for sign in (-1, 1):
+        g = gen(5)
+        Wq, ws = head(V, d, g)
+        ws *= 5.0
+        H = randn(g, B * K, d).bfloat16().abs()
+        for rows in (slice(64, 96), slice(1024, 2048), slice(2500, 2501)):
+            Wq[rows] = 127 * sign
+            ws[rows] = size / (127.0 * d)
+        z = logits_of(Wq, ws, H)
+        assert float(z.abs().max()) > size / 8 and bool(torch.isfinite(z).all())
+        score = beam_scores(g, B, K)
+        want_s, want_p, want_t, _, gap = beams.best_of(z, score, n)
+        assert gap > 4 * beams.LSE_TOL
+        s, p, t = torch.zeros((B, n), device="cuda"), torch.zeros((B, n), dtype=I32, device="cuda"), torch.zeros((B, n), dtype=I32, device="cuda")
+        ctx = beams.context(V, d, batch=B, rows=B * K)
+        ctx.beam_step_int8(Wq, ws, H, score, s, p, t, torch.empty((B * K, V), device="cuda"))
+        assert torch.equal(p.cpu().long(), want_p) and torch.equal(t.cpu().long(), want_t)
+        assert ((s.cpu().double() - want_s).abs() <= beams.score_tol(want_s)).all()
