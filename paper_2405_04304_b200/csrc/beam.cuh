@@ -17,8 +17,6 @@
 
 namespace disco {
 
-constexpr int kBeamChunk = 128;          // logits to a chunk of the pass over given logits
-constexpr int kBeamWarpChunks = 8;       // chunks that a warp takes, so that 32 loads are on their way at once
 constexpr int kBeamStatWarps = 8;
 constexpr int kBeamThreads = 1024;       // of the selection, at most
 constexpr int kBeamCluster = 8;          // CTAs that make the pass over a sequence's logits and select, in one launch

@@ -14,6 +14,21 @@ constexpr int kNFeat = DISCO_NFEAT;
 constexpr unsigned kFullMask = 0xffffffffu;
 constexpr int kNoIndex = 0x7fffffff;
 constexpr int kI8Chunk = 32;   // vocabulary rows per record of soft-max statistics that the 8-bit LM head leaves
+constexpr int kBeamChunk = 128;      // logits to a chunk of the pass over given logits
+constexpr int kBeamWarpChunks = 8;   // chunks to a segment, which a warp of it takes, so that 32 loads are on their way at once
+
+// The statistics of rows of V logits in a context's scratch, in one of two layouts: a pair of floats for each kI8Chunk logits (the 8-bit
+// LM head's), or (given logits) a pair for each segment of a row and, behind those of all rows, a float for each kBeamChunk.
+struct BeamLayout {
+    int i8_chunks, chunks, segs;   // of a row
+    __host__ __device__ explicit BeamLayout(int V)
+        : i8_chunks((V + kI8Chunk - 1) / kI8Chunk), chunks((V + kBeamChunk - 1) / kBeamChunk), segs((chunks + kBeamWarpChunks - 1) / kBeamWarpChunks) {}
+    __host__ __device__ size_t tops_at(size_t rows) const { return rows * segs * 2; }   // in floats
+    __host__ __device__ size_t bytes(size_t rows) const {
+        const size_t i8 = rows * i8_chunks * 2, given = tops_at(rows) + rows * chunks;
+        return (i8 > given ? i8 : given) * sizeof(float);
+    }
+};
 
 // Bounded-wait budget: a wait gives up after this many clock ticks (about 0.05 s by default).  A device
 // variable, one copy per translation unit, so that a test can shorten it (disco_test_hooks) and make a wait

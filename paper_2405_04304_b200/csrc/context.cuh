@@ -43,7 +43,7 @@ struct disco_ctx {
     int8_t* int8_rows;             // hidden rows in 8 bits: [part_rows][int8_pitch]
     float* int8_scale;             //   and their scales
     int int8_pitch;
-    float2* beam_stats;            // [part_rows][ceil(V / kI8Chunk)] soft-max statistics of chunks of logits
+    float2* beam_stats;            // soft-max statistics of part_rows rows of logits: BeamLayout
     int part_slots;                // partials per row the buffers can hold
     void* encode_tiled;            // cuTensorMapEncodeTiled, resolved through the runtime
     void* pointer_attributes;      // cuPointerGetAttributes, the same way

@@ -546,7 +546,7 @@ int disco_create(disco_ctx** out, int V, int d_draft, int d_target, int max_batc
     c->int8_pitch = (std::max(d_draft, d_target) + 15) & ~15;
     device(&c->int8_rows, (size_t)c->part_rows * c->int8_pitch);
     device(&c->int8_scale, (size_t)c->part_rows * sizeof(float));
-    device(&c->beam_stats, (size_t)c->part_rows * ((V + (size_t)kI8Chunk - 1) / kI8Chunk) * sizeof(float2));
+    device(&c->beam_stats, BeamLayout(V).bytes((size_t)c->part_rows));
     auto pinned = [&](size_t bytes) {
         const size_t at = host_bytes;
         host_bytes += (bytes + 255) & ~(size_t)255;

@@ -119,7 +119,7 @@ int launch_int8_head(disco_ctx* c, const Int8Tiling& t, const int8_t* W_q, long 
     p.y = y;
     p.ldy = ldy;
     p.stats = STATS ? c->beam_stats : nullptr;
-    p.chunks = (c->V + kI8Chunk - 1) / kI8Chunk;
+    p.chunks = BeamLayout(c->V).i8_chunks;
     p.status = c->status;
     auto kern = int8_head_kernel<Out, In, STATS, PAIR>;
     static KernelSetup setup;
@@ -188,12 +188,12 @@ BeamParams beam_params(const disco_ctx* c, const void* z, long long ld, int chun
     p.eos = eos;
     p.score = score;
     p.finished = finished;
-    p.chunks = (c->V + chunk - 1) / chunk;
-    p.segs = (p.chunks + kBeamWarpChunks - 1) / kBeamWarpChunks;
-    // (both fit where a pair for each kI8Chunk logits does)
+    const BeamLayout layout(c->V);
+    p.chunks = chunk == kBeamChunk ? layout.chunks : layout.i8_chunks;
+    p.segs = layout.segs;
     p.pairs = c->beam_stats;
     p.sums = c->beam_stats;
-    p.tops = reinterpret_cast<float*>(c->beam_stats + (size_t)B * K * p.segs);
+    p.tops = reinterpret_cast<float*>(c->beam_stats) + layout.tops_at((size_t)B * K);
     p.score_out = score_out;
     p.parent = parent;
     p.token = token;

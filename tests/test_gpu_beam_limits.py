@@ -73,3 +73,12 @@ def test_step_logits_of_any_size(size):
         ctx.beam_step_int8(Wq, ws, H, score, s, p, t, torch.empty((B * K, V), device="cuda"))
         assert torch.equal(p.cpu().long(), want_p) and torch.equal(t.cpu().long(), want_t)
         assert ((s.cpu().double() - want_s).abs() <= beams.score_tol(want_s)).all()
+
+
+# ------------------------------------------------------------------------------------------------ small vocabularies
+@pytest.mark.parametrize("V", [1, 2, 31, 32, 33, 64])
+@pytest.mark.parametrize("B,K", [(8, 8), (64, 4), (4, 64)])
+def test_select_small_vocabularies_with_every_row_of_the_context(V, B, K):
+    """(A row's statistics take more room than one record of the 8-bit head's.)"""
+    g = gen(V * 100 + B)
+    check_select(randn(g, B * K, V), beam_scores(g, B, K), K)
