@@ -367,10 +367,11 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
             if (!is && s_state[k] == 1) s_state[k] = 0;
             s_lse[k] = sum;
             s_top[k] = top;
-            // score = logit + offset, and what fp32 makes of that: a few roundings of numbers of these sizes, and those of the logarithm
+            // score = logit + offset, and what fp32 makes of that: a few roundings of numbers of these sizes and of the logarithm, and
+            // the sum's own rounding, which the logarithm passes on whatever its size (2^-24, where the sum is next to 1)
             const float ln = logf(static_cast<float>(sum));
             s_offset[k] = s_score[k] - (top + ln);
-            s_err[k] = (0x1p-21f * fabsf(s_score[k]) + 0x1p-21f * fabsf(top)) + 0x1p-21f * ln;
+            s_err[k] = (0x1p-21f * fabsf(s_score[k]) + 0x1p-21f * fabsf(top)) + (0x1p-21f * ln + 0x1p-22f);
         }
     }
     __syncthreads();

@@ -82,3 +82,34 @@ def test_select_small_vocabularies_with_every_row_of_the_context(V, B, K):
     """(A row's statistics take more room than one record of the 8-bit head's.)"""
     g = gen(V * 100 + B)
     check_select(randn(g, B * K, V), beam_scores(g, B, K), K)
+
+
+# ------------------------------------------------------------------------------------------------ scores that come near to each other
+def lists_of(ctx, z, score, n):
+    B = score.shape[0]
+    s, p, t = torch.full((B, n), 7.0, device="cuda"), torch.full((B, n), -7, dtype=I32, device="cuda"), torch.full((B, n), -7, dtype=I32, device="cuda")
+    ctx.beam_select(z, score, s, p, t)
+    assert ctx.device_status() == 0
+    return s.cpu().double(), p.cpu().long(), t.cpu().long()
+
+
+@pytest.mark.parametrize("B", [16, 40])                           # one launch, and two
+def test_select_peaked_rows_next_to_zero(B):
+    """Two beams with one likely token each, whose scores differ by less than the rounding of a sum of exponentials next to 1.
+
+    Sums 1 + (m + 0.49) u and 1 + (m - 0.49) u with u = 2^-23: in fp32 they are 1 + m u both.  The second beam's score is 0.9 u lower, so its
+    token is the better one by 0.08 u, while it looks the worse by 0.9 u.  (A sum's own error is 2^-18 of what it has beyond 1: 2^-13 u.)"""
+    V, u = 2048, 2.0 ** -23
+    z, score = torch.full((B, 2, V), -math.inf, device="cuda"), torch.zeros((B, 2), device="cuda")
+    for b in range(B):
+        m = 2 + b
+        z[b, :, 3] = 0.0
+        z[b, 0, 1500], z[b, 1, 1500] = math.log((m + 0.49) * u), math.log((m - 0.49) * u)
+    score[:, 1] = -0.9 * u
+    l = score.double().cpu()[:, :, None] + torch.log_softmax(z.double().cpu(), 2)
+    assert (l[:, 1, 3] - l[:, 0, 3] > 0.05 * u).all()
+    ctx = beams.context(V, batch=B, rows=2 * B)
+    s, p, t = lists_of(ctx, z.view(2 * B, V), score, 1)
+    assert (p == 1).all() and (t == 3).all()
+    s, p, t = lists_of(ctx, z.view(2 * B, V), score, 2)
+    assert (p == torch.tensor([1, 0])).all() and (t == 3).all()
