@@ -372,6 +372,8 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
             const float ln = logf(static_cast<float>(sum));
             s_offset[k] = s_score[k] - (top + ln);
             s_err[k] = (0x1p-21f * fabsf(s_score[k]) + 0x1p-21f * fabsf(top)) + (0x1p-21f * ln + 0x1p-22f);
+            // (an offset beyond what fp32 holds says nothing of the scores: no bound, so nothing of the row is dropped)
+            if (!(fabsf(s_offset[k]) < -DISCO_NEG_INF)) s_err[k] = -DISCO_NEG_INF;
         }
     }
     __syncthreads();

@@ -113,3 +113,17 @@ def test_select_peaked_rows_next_to_zero(B):
     assert (p == 1).all() and (t == 3).all()
     s, p, t = lists_of(ctx, z.view(2 * B, V), score, 2)
     assert (p == torch.tensor([1, 0])).all() and (t == 3).all()
+
+
+@pytest.mark.parametrize("B", [4, 40])                            # one launch, and two
+def test_select_offsets_beyond_fp32(B):
+    """A beam at -3e38 whose logits are all 3e38: score minus logarithm is beyond fp32, the scores themselves (-3e38) are not, and they are
+    better than those of the beam before it.  And the other way round, where the largest logit is far below 0."""
+    V, K, n = 1500, 3, 6
+    z, score = randn(gen(B), B, K, V), torch.empty((B, K), device="cuda")
+    score[:, 0], score[:, 1], score[:, 2] = -3.2e38, -3.0e38, -3.1e38
+    z[:, 1] = 3e38
+    z[::2, 2] = -3e38
+    score[1::2, 2] = 3e38
+    z[1::2, 2] = -2e38
+    check_select(z.view(B * K, V), score, n)
