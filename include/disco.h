@@ -401,8 +401,11 @@ int disco_project_int8(disco_ctx* ctx, const int8_t* W_q, long long ldw, const f
 /*
  * One step of beam search for B sequences of K beams: of all continuations of a sequence the n best by
  *     l[k, v] = score[k] + logits[k, v] - ln sum_w exp(logits[k, w]),
- * best first.  Equal ones: the lower beam, then the lower token.  (A beam's continuations are ordered by their logits; scores of different
- * beams are compared in 64 bits.)
+ * best first, formed and compared in 64 bits as score + (logit - logarithm).  Equal ones: the lower beam, then the lower token.  (So are
+ * continuations whose difference 64 bits do not hold beside the score.)  A logarithm may be off by 2^-18 (2^-20 more for every further
+ * 8192 * (32 / K) logits, the quotient rounded down, or 4096 of more than 32 beams), and score_out by as much beside its own rounding.  Where
+ * continuations of different beams are so near that this could turn them round, the beams' sums are taken again in 64 bits, the same in any
+ * order of the logits.
  *   logits    z_type [B * K, V], rows ldz >= V elements apart (any alignment of its type).  -inf is a token that is not allowed
  *   score     float [B, K]   sums of log-probabilities; a beam at -inf (or NaN, +inf) is dead: it has no continuation and its
  *             logits are not read.  (At the first token all beams but one are.)

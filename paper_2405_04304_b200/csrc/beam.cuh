@@ -5,8 +5,9 @@
 // Every logit is read once, by a pass that leaves the largest of each chunk of neighbouring logits, and sums of exponentials.  (The 8-bit LM
 // head's epilogue leaves the same.)  What follows looks at few logits: the n best lie in the n chunks
 // that come first by (best score, place), since each of those holds a candidate that beats whatever lies in
-// another chunk.  Scores are formed and compared in 64 bits: which of two candidates is the better is a whole number, and the scores of
-// different beams may come as near to each other as they like.
+// another chunk.  Scores are formed and compared in 64 bits: which of two candidates is the better is a whole number.  The sums of
+// exponentials are those of fp32 (beam_ln_err says how far a logarithm may be off) until candidates of different beams come nearer to each
+// other than that; then the beams' sums are taken again, in 64 bits and in any order the same: equal beams stay equal.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -55,6 +56,13 @@ struct BeamDeal {
 // 9.5 / 10.4 / 15.4; with two segments to a warp and more, 20 x 5 of 40011 bf16 13.6 -> 14.9, 1 x 16 of 49152 fp32 11.3 -> 16.7.)
 __host__ __device__ inline bool beam_joined(int B, int K, int segs) { return B <= 32 && K * segs <= 16 * kBeamCluster; }
 
+// How far the logarithm of a row's sum of exponentials in fp32 may be off: relatively, the sum.  In units of 2^-24, for N terms a record, S
+// records a row: exponentials 4 (2 ulp of ex2), their arguments 1.04 log2 N (a t rounded to fp32, of a rounded log2 e, weighs t 2^-t; weighted
+// so, t is log2 N at most), sums 10, what makes good the rounded product 5; records meet with weights exp(top - top') of 6 each, at three
+// levels at most, whose arguments take 2.4 ln S.  Given logits: N = 1024, S <= 1024: 64.  The 8-bit head's, N = 32, S <= 8192, and eight additions to
+// a lane: 60.  A lane that takes its records in several rounds adds a weight and up to eight terms each time: 16.
+__host__ __device__ inline float beam_ln_err(int rounds) { return 0x1p-18f + 0x1p-20f * (rounds - 1); }
+
 struct BeamParams {
     const void* z;               // [B * K, V] logits, rows ld elements apart
     long long ld;
@@ -67,6 +75,7 @@ struct BeamParams {
     float2* sums;                // [B * K][segs] of kBeamWarpChunks chunks each: their largest logit, the sum of exp(z - largest)
     const float2* pairs;         // [B * K][chunks] both for each chunk of kI8Chunk (instead of tops and sums)
     BeamDeal deal;
+    float ln_err;                // beam_ln_err of the deal
     float* score_out;            // [B, n]
     int32_t* parent;
     int32_t* token;
@@ -225,17 +234,43 @@ __device__ __forceinline__ void block_cut(Reach reach, unsigned long long lo, un
     }
 }
 
+// The terms exp(z - top) of a row, by all threads of a block: whole numbers of 2^-62, whose sum is the same in any order.  total: three words
+// of the sum in shared memory, 32 bits apart (2^28 terms at most: no word passes 64 bits).
+// kAtOnce: chains of 64-bit operations beside each other, as far as there are registers.
+template <int kAtOnce, int THREADS, typename T>
+__device__ __forceinline__ void add_exponentials(const T* z, int V, float top, unsigned long long* total) {
+    unsigned __int128 sum = 0;
+#pragma unroll 1
+    for (int v = threadIdx.x; v < V; v += kAtOnce * THREADS) {
+        float x[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) x[i] = v + i * THREADS < V ? load_logit(z + v + i * THREADS) : DISCO_NEG_INF;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) sum += __double2ull_rn(exp(static_cast<double>(x[i]) - static_cast<double>(top)) * 0x1p62);
+    }
+    unsigned long long w[3] = {static_cast<uint32_t>(sum), static_cast<uint32_t>(sum >> 32), static_cast<unsigned long long>(sum >> 64)};
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) w[i] += __shfl_xor_sync(kFullMask, w[i], off);
+        if ((threadIdx.x & 31) == 0) atomicAdd(total + i, w[i]);
+    }
+}
+
 // A CTA to a sequence.  JOINED: a cluster of CTAs, which first of all make the pass over the sequence's logits; one of them goes on.
 //   1  each row's soft-max statistics from its chunks'
 //   2  the pieces that may hold the n best: every piece is known by its best score.  The n-th largest of what the threads have at best is
 //      reached by n pieces at least, and by few more
 //   3  the logits of these pieces, of which those count that reach the same score
-//   4  what is left is scored in 64 bits and ranked by counting
+//   4  what is left is scored in 64 bits and ranked by counting; again, where the order of different beams is within what their sums of
+//      exponentials may be off, with the sums of these beams in 64 bits.  (Seldom: 2^-17 apart.  A beam's
+//      sum takes 12 - 35 us, of 32000 logits by 512 threads - of 49152 by 256.)
 // Up to 4 everything is in fp32 with a bound on its error, from which a piece or a logit is dropped only if it cannot be among the n best:
 // the 64-bit units are too few for a score for every piece (of 32000 logits and 4 beams, 8400 and 4400 cycles for steps 1 and 2 in 64 bits).
 // Where too many are equal for the lists (a call that is full of ties), the cuts are made in 64 bits, by bisection.
-template <typename T, int CHUNK, int THREADS, bool TWO, bool JOINED>
-__global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p) {
+// SIDE: CTAs that are to fit an SM side by side.
+template <typename T, int CHUNK, int THREADS, bool TWO, bool JOINED, int SIDE = 1>
+__global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamParams p) {
     constexpr int kWarps = THREADS / 32;
     __shared__ ulonglong2 s_cand[kBeamList];      // (score, place); in step 3 the logit's bits for the score
     __shared__ int2 s_piece[kBeamPieceList];
@@ -246,6 +281,9 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     __shared__ double s_lse[kBeamMaxBeams];     // the sum of exponentials, then what is taken off a logit
     __shared__ float s_score[kBeamMaxBeams], s_top[kBeamMaxBeams], s_offset[kBeamMaxBeams], s_err[kBeamMaxBeams];
     __shared__ int s_state[kBeamMaxBeams];      // 0: no continuation, 1: expands, 2: finished
+    __shared__ int s_sum64[kBeamMaxBeams];      // the row's sum of exponentials is 0: one of fp32, 1: to be one of 64 bits, 2: that, or none
+    __shared__ unsigned long long s_total[3];
+    __shared__ uint32_t s_unsure;               // how far a score may be off for its sum of exponentials, by the bits
     __shared__ int s_pieces, s_count;
     __shared__ uint32_t s_best[3];
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -316,7 +354,7 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
                     s_state[tid] = !beam_lives(c) ? 0 : over ? 2 : 1;
                 }
                 if (tid < 3) s_best[tid] = 0u;
-                if (tid == 0) s_count = 0, s_pieces = 0;
+                if (tid == 0) s_count = 0, s_pieces = 0, s_unsure = 0u;
             }
 #pragma unroll
             for (int j = 0; j < kBeamItems; ++j) {
@@ -368,10 +406,10 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
             s_lse[k] = sum;
             s_top[k] = top;
             // score = logit + offset, and what fp32 makes of that: a few roundings of numbers of these sizes and of the logarithm, and
-            // the sum's own rounding, which the logarithm passes on whatever its size (2^-24, where the sum is next to 1)
+            // the error of the sum, which the logarithm passes on whatever its size (the sum's own rounding to fp32, 2^-24, among it)
             const float ln = logf(static_cast<float>(sum));
             s_offset[k] = s_score[k] - (top + ln);
-            s_err[k] = (0x1p-21f * fabsf(s_score[k]) + 0x1p-21f * fabsf(top)) + (0x1p-21f * ln + 0x1p-22f);
+            s_err[k] = (0x1p-21f * fabsf(s_score[k]) + 0x1p-21f * fabsf(top)) + (0x1p-21f * ln + p.ln_err);
             // (an offset beyond what fp32 holds says nothing of the scores: no bound, so nothing of the row is dropped)
             if (!(fabsf(s_offset[k]) < -DISCO_NEG_INF)) s_err[k] = -DISCO_NEG_INF;
         }
@@ -379,6 +417,7 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     __syncthreads();
 
     // ---- 2 ----
+    if (tid < p.K) s_sum64[tid] = s_state[tid] == 1 ? 0 : 2;
     // (a warp's rows, the second one where it has two)
     float offset[kRows], err[kRows];
     float low = DISCO_NEG_INF;      // the least that the best of this thread's pieces may score
@@ -429,6 +468,8 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         const float f = z + s_offset[k];
         return f < -DISCO_NEG_INF ? f - (s_err[k] + 0x1p-21f * fabsf(z)) : DISCO_NEG_INF;
     };
+    if (tid < p.K && s_state[tid] == 1 && within(tid, s_top[tid]))       // (and what 64 bits make of numbers of these sizes)
+        atomicMax(&s_unsure, __float_as_uint(p.ln_err + 0x1p-50f * (fabsf(s_score[tid]) + fabsf(s_top[tid]))));
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
         if (!(top[r] > DISCO_NEG_INF) || high(r, top[r]) < floor) continue;      // (so it is with most threads)
@@ -467,10 +508,37 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     auto finish_lse = [&] {
         for (int k = tid; k < p.K; k += THREADS) s_lse[k] = static_cast<double>(s_top[k]) + log(s_lse[k]);
     };
+    auto logit = [&](int k, int v) { return load_logit(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld + v); };
+    // The sums of exponentials that are to be of 64 bits (all threads, behind a barrier).
+    auto sum_again = [&] {
+#pragma unroll 1
+        for (int k = 0; k < p.K; ++k) {
+            if (s_sum64[k] != 1) continue;
+            if (tid == 0) s_total[0] = s_total[1] = s_total[2] = 0ull;
+            __syncthreads();
+            add_exponentials<THREADS == 256 ? 2 : THREADS == 512 && SIDE == 1 ? 4 : 1, THREADS>(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld, p.V, s_top[k], s_total);
+            __syncthreads();
+            if (tid == 0) {
+                const double sum = (static_cast<double>(s_total[2]) * 0x1p64 + static_cast<double>(s_total[1]) * 0x1p32) + static_cast<double>(s_total[0]);
+                s_lse[k] = static_cast<double>(s_top[k]) + log(sum * 0x1p-62);
+                s_sum64[k] = 2;
+            }
+        }
+        __syncthreads();
+    };
+    // Ahead of a cut by scores: those of all rows that the floor leaves, unless that is a single one.
+    auto settle_rows = [&] {
+        const bool left = tid < p.K && (s_state[tid] == 2 || (s_state[tid] == 1 && within(tid, s_top[tid])));
+        if (__syncthreads_count(left) < 2) return;
+        if (left && s_sum64[tid] == 0) s_sum64[tid] = 1;
+        __syncthreads();
+        sum_again();
+    };
     const bool crowded = L > kBeamPieceList;
     if (crowded) {
         finish_lse();
         __syncthreads();
+        settle_rows();
         unsigned long long key[kBeamItems];
 #pragma unroll
         for (int j = 0; j < kBeamItems; ++j)
@@ -504,7 +572,6 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
         v = piece.y + (i - l * width);
         return v < p.V;
     };
-    auto logit = [&](int k, int v) { return load_logit(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld + v); };
     auto place_of = [&](int k, int v) { return (unsigned long long)k << 32 | (unsigned int)v; };
     auto take = [&](unsigned long long x, unsigned long long place) {
         const int at = atomicAdd(&s_count, 1);
@@ -561,6 +628,7 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
             else s_cand[i * THREADS + tid].x = x;
         }
     } else {      // many equal logits
+        settle_rows();
         auto each = [&](auto f) {
             for (int i = tid; i < values; i += THREADS) {
                 int k, v;
@@ -590,21 +658,57 @@ __global__ void __launch_bounds__(THREADS) beam_select_kernel(const BeamParams p
     // ---- 4 ----
     N = s_count;
     const long long out = (long long)b * p.n;
-    for (int i = tid; i < N; i += THREADS) {
-        const ulonglong2 c = s_cand[i];
-        int rank = 0;
+    const double reach = 2.0 * static_cast<double>(__uint_as_float(s_unsure));
+    // Candidates of another beam, no better than c, that may be better if the sums of exponentials are off.
+    auto near = [&](const ulonglong2& c, unsigned long long low, const ulonglong2& o) {
+        return static_cast<int>(o.x >= low) & static_cast<int>(o.x <= c.x) & static_cast<int>(o.y >> 32 != c.y >> 32);
+    };
+    auto low_of = [&](const ulonglong2& c) { return ordered_bits64(from_ordered_bits64(c.x) - reach); };
+    for (;;) {
+        bool unsure = false;
+        for (int i = tid; i < N; i += THREADS) {
+            const ulonglong2 c = s_cand[i];
+            const unsigned long long low = low_of(c);
+            int rank = 0, close = 0;
 #pragma unroll 4
-        for (int j = 0; j < N; ++j) {       // (no branches: with them a candidate costs 140 cycles)
-            const ulonglong2 o = s_cand[j];
-            rank += static_cast<int>(o.x > c.x) | (static_cast<int>(o.x == c.x) & static_cast<int>(o.y < c.y));
+            for (int j = 0; j < N; ++j) {       // (no branches: with them a candidate costs 140 cycles)
+                const ulonglong2 o = s_cand[j];
+                rank += static_cast<int>(o.x > c.x) | (static_cast<int>(o.x == c.x) & static_cast<int>(o.y < c.y));
+                close |= near(c, low, o);
+            }
+            if (rank < p.n) {       // (what is read of the beams has been read: the outputs may take the inputs' place)
+                const int parent = static_cast<int>(c.y >> 32), token = static_cast<int>(c.y & 0xffffffffull);
+                p.score_out[out + rank] = static_cast<float>(from_ordered_bits64(c.x));
+                p.parent[out + rank] = parent;
+                p.token[out + rank] = token;
+                if (p.finished_out) p.finished_out[out + rank] = token == p.eos || s_state[parent] == 2;
+                unsure = unsure || close != 0;
+            }
         }
-        if (rank < p.n) {       // (what is read of the beams has been read: the outputs may take the inputs' place)
-            const int parent = static_cast<int>(c.y >> 32), token = static_cast<int>(c.y & 0xffffffffull);
-            p.score_out[out + rank] = static_cast<float>(from_ordered_bits64(c.x));
-            p.parent[out + rank] = parent;
-            p.token[out + rank] = token;
-            if (p.finished_out) p.finished_out[out + rank] = token == p.eos || s_state[parent] == 2;
+        if (p.K == 1 || !__syncthreads_or(unsure)) break;
+        // Once more with sums of 64 bits of the beams that matter, if they are not of 64 bits already (so as many rounds as beams, at most).
+        bool more = false;
+        for (int i = tid; i < N; i += THREADS) {
+            const ulonglong2 c = s_cand[i];
+            const unsigned long long low = low_of(c);
+            const int k = static_cast<int>(c.y >> 32);
+            for (int j = 0; j < N; ++j) {
+                const ulonglong2 o = s_cand[j];
+                const int l = static_cast<int>(o.y >> 32);
+                if (!near(c, low, o) || (s_sum64[k] == 2 && s_sum64[l] == 2)) continue;
+                if (s_sum64[k] == 0) s_sum64[k] = 1;
+                if (s_sum64[l] == 0) s_sum64[l] = 1;
+                more = true;
+            }
         }
+        if (!__syncthreads_or(more)) break;
+        sum_again();
+        for (int i = tid; i < N; i += THREADS) {
+            const unsigned long long place = s_cand[i].y;
+            const int k = static_cast<int>(place >> 32);
+            if (s_state[k] == 1) s_cand[i].x = score_of(k, logit(k, static_cast<int>(place & 0xffffffffull)));
+        }
+        __syncthreads();
     }
     for (int i = N + tid; i < p.n; i += THREADS) {
         p.score_out[out + i] = DISCO_NEG_INF;

@@ -206,8 +206,13 @@ int launch_beam_select(disco_ctx* c, BeamParams p, cudaStream_t st) {
     int warps = BeamDeal::warps(p.K, p.chunks, p.n);
     if (JOINED && warps == 8 && p.K * p.segs > 8 * kBeamCluster) warps = 16;      // (a warp to each segment)
     p.deal = BeamDeal::make(p.K, p.chunks, warps);
+    const int lanes = 32 * p.deal.share;
+    p.ln_err = beam_ln_err(CHUNK == kBeamChunk ? (p.segs + lanes - 1) / lanes : p.deal.merged);
+    // Sixteen warps to a sequence: no register goes to memory where a CTA has an SM to itself; more sequences than SMs are the faster two by
+    // two (us a pass, one -> two: 64 x 8 of 49152 27.4 -> 28.2, 160 x 4 on a head of 32000 x 768 48.7 -> 45.9).
+    const bool few = JOINED || p.B <= c->sm_count;
     auto kern = warps == 8    ? beam_select_kernel<T, CHUNK, 256, false, JOINED>
-                : warps == 16 ? beam_select_kernel<T, CHUNK, 512, false, JOINED>
+                : warps == 16 ? (few ? beam_select_kernel<T, CHUNK, 512, false, JOINED> : beam_select_kernel<T, CHUNK, 512, false, JOINED, 2>)
                 : p.deal.two  ? beam_select_kernel<T, CHUNK, 1024, true, JOINED>
                               : beam_select_kernel<T, CHUNK, 1024, false, JOINED>;
     cudaLaunchConfig_t cfg{};

@@ -127,3 +127,124 @@ def test_select_offsets_beyond_fp32(B):
     score[1::2, 2] = 3e38
     z[1::2, 2] = -2e38
     check_select(z.view(B * K, V), score, n)
+
+
+def best_by_sorted_sums(z, score, n, finished=None, eos=-1):
+    """best_of in 64 bits with each row's exponentials added in the order of their size: rows of the same logits, wherever these stand, get the
+    same sum.  Differences of neighbours of different beams are 2^-40 at least, or none: 64-bit sums are good to less than 2^-46."""
+    B, K = score.shape
+    z = z.double().reshape(B, K, -1).cpu()
+    lse = torch.logsumexp(z.sort(2).values, 2, keepdim=True)
+    l = score.double().cpu()[:, :, None] + (z - lse)
+    if finished is not None:
+        for b, k in finished.cpu().nonzero().tolist():
+            l[b, k] = -math.inf
+            l[b, k, eos] = float(score[b, k])
+    V = z.shape[2]
+    flat = l.reshape(B, K * V)
+    at = torch.argsort(flat, dim=1, descending=True, stable=True)[:, :n + 1]
+    s = flat.gather(1, at)
+    gap = (s[:, :-1] - s[:, 1:])[(at[:, :-1] // V != at[:, 1:] // V)]
+    assert (gap[gap != 0] > 2.0 ** -40).all()
+    return s[:, :n], at[:, :n] // V, at[:, :n] % V
+
+
+def check_near(z, score, n, want, finished=None, eos=-1):
+    B, K = score.shape
+    V = z.shape[-1]
+    ctx = beams.context(V, batch=B, rows=B * K)
+    s, p, t = torch.full((B, n), 7.0, device="cuda"), torch.full((B, n), -7, dtype=I32, device="cuda"), torch.full((B, n), -7, dtype=I32, device="cuda")
+    ctx.beam_select(z.view(B * K, V), score, s, p, t, finished=finished, eos=eos)
+    assert ctx.device_status() == 0
+    assert torch.equal(p.cpu().long(), want[1]) and torch.equal(t.cpu().long(), want[2])
+    assert ((s.cpu().double() - want[0]).abs() <= beams.score_tol(want[0])).all()
+
+
+def near_scores(z, B, K):
+    """Scores with which the beams' best continuations are equal but for the rounding of the scores, 2^-23 at most."""
+    z = z.double().view(B, K, -1)
+    best = (z.amax(2) - torch.logsumexp(z, 2))
+    return (-3.0 - best).float()
+
+
+@pytest.mark.parametrize("z_type", [F32, BF16, F16])
+@pytest.mark.parametrize("B,K,n,V", [(8, 2, 1, 500), (8, 4, 4, 5000), (40, 4, 8, 2500), (4, 16, 16, 9001), (2, 40, 30, 700), (3, 64, 128, 2050), (1, 3, 5, 151936)])
+def test_select_beams_nearer_than_fp32_sums(z_type, B, K, n, V):
+    g = gen(B * 7 + K + V)
+    z = (randn(g, B * K, V) * 1.5).to(z_type)
+    score = near_scores(z, B, K)
+    check_near(z, score, n, best_by_sorted_sums(z, score, n))
+
+
+@pytest.mark.parametrize("B", [6, 40])
+def test_select_ended_beams_next_to_others(B):
+    """An ended beam's score is exact; a living one's continuation comes as near to it as fp32 scores allow."""
+    g = gen(B)
+    K, V, n = 4, 3000, 4
+    z = randn(g, B * K, V) * 1.5
+    score, fin = near_scores(z, B, K), torch.zeros((B, K), dtype=beams.U8, device="cuda")
+    fin[:, 1] = 1
+    # (scores one by one: of the same logits, the first of many near ones that is not a tie)
+    score[:, 1] = (score[:, 0].double() + z.double().view(B, K, V)[:, 0].amax(1) - torch.logsumexp(z.double().view(B, K, V)[:, 0], 1)).float()
+    check_near(z, score, n, best_by_sorted_sums(z, score, n, fin, 7), fin, 7)
+
+
+def permuted(g, B, K, V, values):
+    """K rows of the same logits, each in an order of its own."""
+    z = torch.empty((B, K, V))
+    for b in range(B):
+        for k in range(K):
+            z[b, k] = values[b][torch.randperm(V, generator=g)]
+    return z.cuda()
+
+
+@pytest.mark.parametrize("z_type", [F32, BF16])
+@pytest.mark.parametrize("B,K,n,V", [(4, 4, 4, 5000), (40, 3, 6, 1500), (2, 16, 20, 3001), (1, 50, 100, 700)])
+def test_select_equal_beams_with_their_logits_in_another_order(z_type, B, K, n, V):
+    """Equal continuations of different beams: the lower beam, in whatever order its logits were added."""
+    g = gen(V + K)
+    z = permuted(g, B, K, V, [torch.randn(V, generator=g) * 1.5 for _ in range(B)]).to(z_type).view(B * K, V)
+    score = torch.full((B, K), -2.5, device="cuda")
+    check_near(z, score, n, best_by_sorted_sums(z, score, n))
+
+
+@pytest.mark.parametrize("B", [2, 40])
+@pytest.mark.parametrize("K,n,V,values", [(3, 100, 6000, 3), (3, 4, 6000, 3), (2, 128, 30000, 40), (4, 20, 70000, 2), (1, 30, 30000, 2), (40, 128, 1500, 2)])
+def test_select_equal_beams_full_of_ties(K, n, V, values, B):
+    """The same with few values: more pieces and more logits at the cut than the lists hold."""
+    if B * K * V > 9_000_000:
+        B = max(1, 9_000_000 // (K * V))
+    g = gen(V + K + values)
+    z = permuted(g, B, K, V, [torch.randint(0, values, (V,), generator=g).float() for _ in range(B)]).view(B * K, V)
+    score = torch.full((B, K), -1.5, device="cuda")
+    score[:, K // 2:] -= 2.0 ** -20
+    check_near(z, score, n, best_by_sorted_sums(z, score, n))
+
+
+def test_select_equal_logits_before_a_better_beam():
+    """The n-th best and what comes behind it are equal continuations of one beam; a third, of another beam, may be better than both."""
+    g = gen(77)
+    B, V = 40, 2000
+    z = randn(g, 2 * B, V)
+    top = z.amax(1)
+    z[::2, 1000] = z[::2, 10] = z[::2, 500] = top[::2] + 1.0
+    score = near_scores(z, B, 2)
+    for n in (1, 2):
+        check_near(z, score, n, best_by_sorted_sums(z, score, n))
+
+
+@pytest.mark.parametrize("V,d,B,K,n", [(5000, 256, 3, 4, 8), (700, 64, 2, 33, 20), (9001, 512, 40, 4, 4)])
+def test_step_beams_nearer_than_fp32_sums(V, d, B, K, n):
+    g = gen(V)
+    Wq, ws = head(V, d, g)
+    ws *= 55.0 / math.sqrt(d)
+    H = randn(g, B * K, d).bfloat16()
+    H[1] = H[0]
+    z = logits_of(Wq, ws, H)
+    score = near_scores(z, B, K)
+    want = best_by_sorted_sums(z, score, n)
+    s, p, t = torch.zeros((B, n), device="cuda"), torch.zeros((B, n), dtype=I32, device="cuda"), torch.zeros((B, n), dtype=I32, device="cuda")
+    ctx = beams.context(V, d, batch=B, rows=B * K)
+    ctx.beam_step_int8(Wq, ws, H, score, s, p, t, torch.empty((B * K, V), device="cuda"))
+    assert torch.equal(p.cpu().long(), want[1]) and torch.equal(t.cpu().long(), want[2])
+    assert ((s.cpu().double() - want[0]).abs() <= beams.score_tol(want[0])).all()
