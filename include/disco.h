@@ -108,7 +108,8 @@ int disco_set_kernel_path(disco_ctx* ctx, int which);
  *                       status word (0 restores the default of about 0.05 s); applies to every context of the
  *                       process
  *   withhold_records    non-zero: the draft step (the tensor-core kernel)
- *                       makes its finishing warps look for per-CTA records that no CTA publishes, so that
+ *                       makes its finishing warps look for per-CTA records that no CTA publishes, and the
+ *                       product of an 8-bit head looks for tiles that it does not load, so that
  *                       their wait runs out.  The kernel still returns by itself; its outputs are then
  *                       meaningless and the context must be destroyed (see DISCO_ERR_TIMEOUT).
  * Nothing traps, faults or waits without bound in either setting. */

@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
         // (more pieces than the list holds, so n at least have been found)
         floor = __double2float_rd(from_ordered_bits64(t));
         __syncthreads();
-        L = s_pieces;
+        L = min(s_pieces, kBeamPieceList);      // (a matter of course, unless the statistics are those of a product whose wait ran out)
     }
 
     // ---- 3 ----
@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
     __syncthreads();
 
     // ---- 4 ----
-    N = s_count;
+    N = min(s_count, kBeamList);      // (the same)
     const long long out = (long long)b * p.n;
     const double reach = 2.0 * static_cast<double>(__uint_as_float(s_unsure));
     // Candidates of another beam, no better than c, that may be better if the sums of exponentials are off.

@@ -189,6 +189,16 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, int* s
     return mbar_wait(smem_addr(bar), parity, status);
 }
 
+// Wait until what this thread has in flight itself is there, ahead of its CTA's end: whatever wait has run out before, so with a budget of
+// its own, from t0 on.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, long long t0, int* status) {
+    while (!mbar_try_wait(bar, parity)) {
+        if (clock64() - t0 <= kDefaultWaitBudgetClocks) continue;
+        record_status(status, DISCO_ERR_TIMEOUT);
+        return;
+    }
+}
+
 // For a barrier at which threads of another CTA of the cluster arrive.
 __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, int* status) {
     const long long t0 = clock64();

@@ -120,6 +120,7 @@ int launch_int8_head(disco_ctx* c, const Int8Tiling& t, const int8_t* W_q, long 
     p.ldy = ldy;
     p.stats = STATS ? c->beam_stats : nullptr;
     p.chunks = BeamLayout(c->V).i8_chunks;
+    p.withhold = c->test_stamp_skew != 0;
     p.status = c->status;
     auto kern = int8_head_kernel<Out, In, STATS, PAIR>;
     static KernelSetup setup;

@@ -298,6 +298,7 @@ struct Int8Params {
     long long ldy;
     float2* stats;             // [R][chunks] (largest logit of the chunk, sum of exp(z - largest)), or null
     int chunks;
+    int withhold;              // disco_test_hooks: no tile is loaded
     int* status;
 };
 
@@ -405,6 +406,8 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, int (&r)[16]) {
 //   * warp 0    producer: a box of TR vocabulary rows x 128 k and one of the tile's hidden rows per stage
 //   * warp 1    MMA issuer: M = 128 (twice for more than 128 vocabulary rows), N = hidden rows of the tile, K = 32
 //   * warps 2+  epilogue: a thread owns a vocabulary row and walks over the hidden rows
+// Where a wait runs out, producer and issuer stop, and leave once their loads and products in flight are done; the epilogue's warps go
+// through their items all the same (their barriers need all of them), with results that mean nothing.
 template <typename Out, typename In, bool STATS, bool PAIR>
 __global__ void __launch_bounds__(kI8Threads, 1)
 int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_constant__ CUtensorMap tmap_X, const Int8Params p) {
@@ -420,7 +423,8 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
     uint64_t* tmem_full = empty + kI8MaxStages;
     uint64_t* tmem_empty = tmem_full + 2;
     uint64_t* rows_full = tmem_empty + 2;
-    uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(rows_full + 1);
+    uint64_t* done = rows_full + 1;        // all products
+    uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(done + 1);
 
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
@@ -444,6 +448,7 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
             mbar_init(&tmem_empty[b], PAIR ? 2 * kI8EpiWarps : kI8EpiWarps);
         }
         mbar_init(rows_full, kI8EpiWarps);
+        mbar_init(done, 1);
         fence_mbar_init();
         prefetch_tensormap(&tmap_W);
         if (!FEW) prefetch_tensormap(&tmap_X);
@@ -480,7 +485,8 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
             // requested at once, the hidden rows of the same stages behind the wait for that kernel.
             // (FEW: what ran before this may have written the head.)
             if (FEW) asm volatile("griddepcontrol.wait;" ::: "memory");
-            const int pre = item < items ? min(p.ring.stages, KB) : 0;
+            const int end = p.withhold ? 0 : items;
+            const int pre = item < end ? min(p.ring.stages, KB) : 0;
             for (int n = 0; n < pre; ++n) {
                 if (leader) mbar_arrive_expect_tx(full0 + n * 8, expected);
                 load(w0 + n * p.ring.w_bytes, &tmap_W, n * kI8BK, item / t.MT * t.TR + v_own, n);
@@ -490,10 +496,12 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
             for (int n = 0; !FEW && n < pre; ++n) load(x0 + n * p.ring.x_bytes, &tmap_X, n * kI8BK, first_row(item), n);
             int stage = pre == p.ring.stages ? 0 : pre, phase = pre == p.ring.stages ? 1 : 0;
             int k = pre * kI8BK;
-            for (; item < items; item += workers, k = 0) {
+            bool ok = true;
+            for (; ok && item < end; item += workers, k = 0) {
                 const int v0 = item / t.MT * t.TR + v_own, r0 = first_row(item);
                 for (; k < k_end; k += kI8BK) {
-                    mbar_wait(empty0 + stage * 8, phase ^ 1, p.status);
+                    ok = mbar_wait(empty0 + stage * 8, phase ^ 1, p.status);
+                    if (!ok) break;
                     if (leader) mbar_arrive_expect_tx(full0 + stage * 8, expected);
                     load(w0 + stage * p.ring.w_bytes, &tmap_W, k, v0, stage);
                     if (!FEW) load(x0 + stage * p.ring.x_bytes, &tmap_X, k, r0, stage);
@@ -501,10 +509,20 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
                 }
             }
             if constexpr (PAIR) {   // the leader's arrivals at this CTA's barriers are all in before it leaves
+                int s = stage, ph = phase;
                 for (int n = 0; n < p.ring.stages; ++n) {
-                    mbar_wait(empty0 + stage * 8, phase ^ 1, p.status);
-                    if (++stage == p.ring.stages) stage = 0, phase ^= 1;
+                    ok = mbar_wait(empty0 + s * 8, ph ^ 1, p.status) && ok;
+                    if (++s == p.ring.stages) s = 0, ph ^= 1;
                 }
+            }
+            // The last load of each slot is in.  (A slot without one passes: its barrier is in its first phase, and the phase before that is
+            // what is asked for.  Those of a pair's second CTA are counted at the leader, which waits for both; where the two have not got
+            // equally far, nothing counts them, and only then there is a pause of a millisecond instead.)
+            const long long t0 = clock64();
+            for (int s = 0; leader && s < p.ring.stages; ++s) mbar_drain(full0 + s * 8, s < stage ? phase : phase ^ 1, t0, p.status);
+            if constexpr (PAIR) {
+                while (!ok && clock64() - t0 < 2000000) {}
+                if (!leader) mbar_drain(smem_addr(done), 0, t0, p.status);
             }
         }
     } else if (warp == 1) {
@@ -524,21 +542,24 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
             const uint32_t w_step = (uint32_t)p.ring.w_bytes >> 4, x_step = (FEW ? (uint32_t)t.N * kI8BK : (uint32_t)p.ring.x_bytes) >> 4;   // descriptor units
             uint64_t w_desc = w_desc0, x_desc = x_desc0;
             int stage = 0, phase = 0, it = 0;
+            bool ok = true;
             if (FEW) {
-                mbar_wait(rows_full, 0, p.status);
+                ok = mbar_wait(rows_full, 0, p.status);
                 tc_fence_after();
             }
-            for (int item = worker; item < items; item += workers, ++it) {
+            for (int item = worker; ok && item < items; item += workers, ++it) {
                 if (FEW) x_desc = x_desc0;
                 const int b = t.bufs == 2 ? it & 1 : 0;
                 const uint32_t parity = ((t.bufs == 2 ? it >> 1 : it) & 1) ^ 1;
-                if constexpr (PAIR) mbar_wait_cluster(smem_addr(&tmem_empty[b]), parity, p.status);
-                else mbar_wait(&tmem_empty[b], parity, p.status);
+                if constexpr (PAIR) ok = mbar_wait_cluster(smem_addr(&tmem_empty[b]), parity, p.status);
+                else ok = mbar_wait(&tmem_empty[b], parity, p.status);
+                if (!ok) break;
                 tc_fence_after();
                 idesc = umma_idesc_i8(columns(item), PAIR ? 256 : 128);
                 const uint32_t d_tmem = tmem_base + b * t.blocks * t.cols;
                 for (int kb = 0; kb < KB; ++kb) {
-                    mbar_wait(full0 + stage * 8, phase, p.status);
+                    ok = mbar_wait(full0 + stage * 8, phase, p.status);
+                    if (!ok) break;
                     tc_fence_after();
 #pragma unroll
                     for (int k = 0; k < 4; ++k)       // 32 k elements = 32 bytes = 2 descriptor units
@@ -556,8 +577,10 @@ int8_head_kernel(const __grid_constant__ CUtensorMap tmap_W, const __grid_consta
                         if (!FEW) x_desc = x_desc0;
                     }
                 }
-                commit(smem_addr(&tmem_full[b]));
+                if (ok) commit(smem_addr(&tmem_full[b]));
             }
+            commit(smem_addr(done));
+            mbar_drain(smem_addr(done), 0, clock64(), p.status);
         }
     } else {
         // ------------------------------ epilogue ------------------------------
