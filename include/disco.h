@@ -416,7 +416,7 @@ int disco_project_int8(disco_ctx* ctx, const int8_t* W_q, long long ldw, const f
  * Outputs:
  *   score_out [B, n], parent [B, n] (the beam), token [B, n]; finished_out uint8 [B, n] or NULL: the parent had ended, or token == eos.
  *   Places that no continuation is left for get (-inf, -1, -1, 0).  With n == K, score_out may be score and finished_out finished.
- * 1 <= K <= DISCO_MAX_BEAMS, 1 <= n <= DISCO_MAX_KEPT.
+ * 1 <= K <= DISCO_MAX_BEAMS, 1 <= n <= DISCO_MAX_KEPT, V <= 2^28 (DISCO_ERR_UNSUPPORTED_SHAPE).
  */
 int disco_beam_select(disco_ctx* ctx, const void* logits, int z_type, long long ldz, int B, int K, const float* score,
                       const uint8_t* finished, int eos, int n, float* score_out, int32_t* parent, int32_t* token,

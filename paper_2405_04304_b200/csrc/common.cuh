@@ -15,6 +15,7 @@ constexpr unsigned kFullMask = 0xffffffffu;
 constexpr int kNoIndex = 0x7fffffff;
 constexpr int kI8Chunk = 32;   // vocabulary rows per record of soft-max statistics that the 8-bit LM head leaves
 constexpr int kBeamChunk = 128;      // logits to a chunk of the pass over given logits
+constexpr int kBeamMaxVocab = 1 << 28;   // logits to a beam: those of the pieces that are looked into (512 of V / 128 + 128 at most) are counted in 32 bits
 constexpr int kBeamWarpChunks = 8;   // chunks to a segment, which a warp of it takes, so that 32 loads are on their way at once
 
 // The statistics of rows of V logits in a context's scratch, in one of two layouts: a pair of floats for each kI8Chunk logits (the 8-bit
@@ -22,7 +23,7 @@ constexpr int kBeamWarpChunks = 8;   // chunks to a segment, which a warp of it 
 struct BeamLayout {
     int i8_chunks, chunks, segs;   // of a row
     __host__ __device__ explicit BeamLayout(int V)
-        : i8_chunks((V + kI8Chunk - 1) / kI8Chunk), chunks((V + kBeamChunk - 1) / kBeamChunk), segs((chunks + kBeamWarpChunks - 1) / kBeamWarpChunks) {}
+        : i8_chunks((V - 1) / kI8Chunk + 1), chunks((V - 1) / kBeamChunk + 1), segs((chunks - 1) / kBeamWarpChunks + 1) {}
     __host__ __device__ size_t tops_at(size_t rows) const { return rows * segs * 2; }   // in floats
     __host__ __device__ size_t bytes(size_t rows) const {
         const size_t i8 = rows * i8_chunks * 2, given = tops_at(rows) + rows * chunks;

@@ -167,7 +167,7 @@ int project(disco_ctx* c, const int8_t* W_q, long long ldw, const float* w_scale
 int check_beams(const disco_ctx* c, int B, int K, int n, const float* score, const uint8_t* finished, int eos, const float* score_out,
                 const int32_t* parent, const int32_t* token, const uint8_t* finished_out) {
     if (!score || !score_out || !parent || !token || B < 1 || K < 1 || n < 1) return DISCO_ERR_INVALID_ARG;
-    if (K > DISCO_MAX_BEAMS || n > DISCO_MAX_KEPT) return DISCO_ERR_UNSUPPORTED_SHAPE;
+    if (K > DISCO_MAX_BEAMS || n > DISCO_MAX_KEPT || c->V > kBeamMaxVocab) return DISCO_ERR_UNSUPPORTED_SHAPE;
     if (finished ? eos < 0 : eos < -1) return DISCO_ERR_INVALID_ARG;
     if (eos >= c->V) return DISCO_ERR_INVALID_ARG;
     if (!aligned(score, 4) || !aligned(score_out, 4) || !aligned(parent, 4) || !aligned(token, 4)) return DISCO_ERR_INVALID_ARG;

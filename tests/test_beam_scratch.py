@@ -1,4 +1,5 @@
-"""Host-only check of where the soft-max statistics of rows of logits lie (compiled from the kernels' own header, run on the CPU)."""
+"""Host-only checks of where the soft-max statistics of rows of logits lie, and of counts of logits (compiled from the kernels' own header,
+run on the CPU)."""
 from test_beam_rules import _run
 
 _LAYOUT = r"""
@@ -20,10 +21,19 @@ int main() {
             }
             if (!ok) return std::printf("V %d, %d rows\n", V, room), 1;
         }
+    // the logits of as many pieces as are looked into, by the deals of all numbers of beams
+    for (int K = 1; K <= DISCO_MAX_BEAMS; ++K)
+        for (int chunk : {kI8Chunk, kBeamChunk}) {
+            const BeamLayout l(kBeamMaxVocab);
+            const int chunks = chunk == kI8Chunk ? l.i8_chunks : l.chunks, warps = BeamDeal::warps(K, chunks, 1);
+            const BeamDeal d = BeamDeal::make(K, chunks, warps);
+            const long long width = (long long)d.merged * chunk, values = kBeamPieceList * width + 8 * kBeamThreads;
+            if (values > 0x7fffffffll || d.pieces * width + 8 * kBeamThreads > 0x7fffffffll) return std::printf("K %d chunk %d\n", K, chunk), 2;
+        }
     return 0;
 }
 """
 
 
-def test_statistics_lie_within_the_contexts_scratch(tmp_path):
+def test_statistics_lie_within_the_contexts_scratch_and_counts_within_32_bits(tmp_path):
     _run(tmp_path, _LAYOUT)

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import test_gpu_beams as beams
+from paper_2405_04304_b200 import binding
 from test_gpu_beams import BF16, F16, F32, I32, beam_scores, check_select, gen, head, logits_of, randn
 
 pytestmark = pytest.mark.gpu
@@ -248,3 +249,28 @@ def test_step_beams_nearer_than_fp32_sums(V, d, B, K, n):
     ctx.beam_step_int8(Wq, ws, H, score, s, p, t, torch.empty((B * K, V), device="cuda"))
     assert torch.equal(p.cpu().long(), want[1]) and torch.equal(t.cpu().long(), want[2])
     assert ((s.cpu().double() - want[0]).abs() <= beams.score_tol(want[0])).all()
+
+
+# ------------------------------------------------------------------------------------------------ large vocabularies
+def test_select_largest_vocabulary_and_one_beyond_it():
+    V, K, n = 1 << 28, 34, 5
+    z = torch.empty((K, V), dtype=F16, device="cuda").uniform_(-4.0, 0.0)
+    at = [(33, V - 1), (0, 0), (32, 1 << 27), (33, 12345), (5, (1 << 28) - 4097)]
+    for i, (k, v) in enumerate(at):
+        z[k, v] = 60.0 - i
+    score = torch.linspace(-1.0, -2.0, K, device="cuda")[None].contiguous()
+    lse = torch.stack([torch.logsumexp(row.double(), 0) for row in z])
+    l = [float(score[0, k].double() + (z[k, v].double() - lse[k])) for k, v in at]
+    order = sorted(range(n), key=lambda i: -l[i])
+    assert all(l[a] - l[b] > 1e-3 for a, b in zip(order, order[1:]))
+    ctx = beams.context(V, d=8, batch=1, rows=K)
+    s, p, t = lists_of(ctx, z, score, n)
+    assert list(zip(p[0].tolist(), t[0].tolist())) == [at[i] for i in order]
+    assert all(abs(float(s[0, j]) - l[i]) < 2.0 ** -20 * V / 4096 for j, i in enumerate(order))
+    ctx.close()
+    more = beams.context(V + 1, d=8, batch=1, rows=1)
+    vp, UNS = lambda t: t.data_ptr(), binding.ERR_UNSUPPORTED_SHAPE
+    s, p = torch.zeros(1, device="cuda"), torch.zeros(1, dtype=I32, device="cuda")
+    assert more._lib.disco_beam_select(more._h, vp(z), 2, V + 1, 1, 1, vp(s), None, -1, 1, vp(s), vp(p), vp(p), None, None) == UNS
+    assert more.launch_count() == 0
+    more.close()
