@@ -234,19 +234,49 @@ __device__ __forceinline__ void block_cut(Reach reach, unsigned long long lo, un
     }
 }
 
-// The terms exp(z - top) of a row, by all threads of a block: whole numbers of 2^-62, whose sum is the same in any order.  total: three words
-// of the sum in shared memory, 32 bits apart (2^28 terms at most: no word passes 64 bits).
-// kAtOnce: chains of 64-bit operations beside each other, as far as there are registers.
+// 1 + exp(x - top) by its bits, x <= top: less those of 1, the term as a whole number of 2^-52.  2^t = 2^n 2^f with t = (x - top) log2 e, n the
+// nearest integer, and 2^f = exp(f ln 2) by its Taylor polynomial of degree 11, off by 0.347^12 / 12! = 2^-47 at most.
+constexpr unsigned long long kOneBits = 0x3ff0000000000000ull;
+__device__ __forceinline__ unsigned long long one_and_exponential(float x, double top) {
+    const double t = (static_cast<double>(x) - top) * 1.4426950408889634074;
+    constexpr double kWhole = 0x1.8p52;      // (the sum with it leaves the nearest integer in the low bits)
+    const double r = t + kWhole, f = t - (r - kWhole);
+    constexpr double kLn2 = 0.69314718055994530942;
+    constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4, c5 = c4 * kLn2 / 5, c6 = c5 * kLn2 / 6, c7 = c6 * kLn2 / 7,
+                     c8 = c7 * kLn2 / 8, c9 = c8 * kLn2 / 9, c10 = c9 * kLn2 / 10, c11 = c10 * kLn2 / 11;
+    double p = c11;
+    p = fma(p, f, c10), p = fma(p, f, c9), p = fma(p, f, c8), p = fma(p, f, c7), p = fma(p, f, c6), p = fma(p, f, c5);
+    p = fma(p, f, c4), p = fma(p, f, c3), p = fma(p, f, c2), p = fma(p, f, c1), p = fma(p, f, 1.0);
+    p = __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
+    return t > -64.0 ? static_cast<unsigned long long>(__double_as_longlong(1.0 + p)) : kOneBits;      // (-inf: nothing)
+}
+
+// The sum of the terms exp(z - top) of a row, by all threads of a block, as whole numbers of 2^-52: the same in any order, and off by no more than
+// sums in 64 bits are.  total: three words of it in shared memory, 32 bits apart (2^28 terms at most: no word passes 64 bits).
+// kAtOnce logits of a thread on their way while as many are at work, as far as there are registers.
 template <int kAtOnce, int THREADS, typename T>
 __device__ __forceinline__ void add_exponentials(const T* z, int V, float top, unsigned long long* total) {
     unsigned __int128 sum = 0;
+    float next[kAtOnce];
+    auto load = [&](int v) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) next[i] = v + i * THREADS < V ? load_logit(z + v + i * THREADS) : DISCO_NEG_INF;
+    };
+    load(threadIdx.x);
 #pragma unroll 1
-    for (int v = threadIdx.x; v < V; v += kAtOnce * THREADS) {
-        float x[kAtOnce];
+    for (int v = threadIdx.x; v < V;) {
+        unsigned long long some = 0ull;      // 2048 terms of 2^52 at most, modulo 2^64
+        int n = 0;
+#pragma unroll 1
+        for (; v < V && n < 2048; v += kAtOnce * THREADS, n += kAtOnce) {
+            float x[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) x[i] = v + i * THREADS < V ? load_logit(z + v + i * THREADS) : DISCO_NEG_INF;
+            for (int i = 0; i < kAtOnce; ++i) x[i] = next[i];
+            load(v + kAtOnce * THREADS);
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) sum += __double2ull_rn(exp(static_cast<double>(x[i]) - static_cast<double>(top)) * 0x1p62);
+            for (int i = 0; i < kAtOnce; ++i) some += one_and_exponential(x[i], static_cast<double>(top));
+        }
+        sum += some - n * kOneBits;
     }
     unsigned long long w[3] = {static_cast<uint32_t>(sum), static_cast<uint32_t>(sum >> 32), static_cast<unsigned long long>(sum >> 64)};
 #pragma unroll
@@ -263,14 +293,14 @@ __device__ __forceinline__ void add_exponentials(const T* z, int V, float top, u
 //      reached by n pieces at least, and by few more
 //   3  the logits of these pieces, of which those count that reach the same score
 //   4  what is left is scored in 64 bits and ranked by counting; again, where the order of different beams is within what their sums of
-//      exponentials may be off, with the sums of these beams in 64 bits.  (Seldom: 2^-17 apart.  A beam's
-//      sum takes 12 - 35 us, of 32000 logits by 512 threads - of 49152 by 256.)
+//      exponentials may be off, with the sums of these beams in 64 bits.  (Seldom, 2^-17 apart: of 64 kept of 16 beams 1.5 %
+//      of the sequences, of 8 of 8 below 0.1 %.  A beam's sum takes 9 - 19 us, of 32000 logits by 512 threads - of 49152 by 256.)
 // Up to 4 everything is in fp32 with a bound on its error, from which a piece or a logit is dropped only if it cannot be among the n best:
 // the 64-bit units are too few for a score for every piece (of 32000 logits and 4 beams, 8400 and 4400 cycles for steps 1 and 2 in 64 bits).
 // Where too many are equal for the lists (a call that is full of ties), the cuts are made in 64 bits, by bisection.
 // SIDE: CTAs that are to fit an SM side by side.
 template <typename T, int CHUNK, int THREADS, bool TWO, bool JOINED, int SIDE = 1>
-__global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamParams p) {
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_select_kernel(const BeamParams p) {
     constexpr int kWarps = THREADS / 32;
     __shared__ ulonglong2 s_cand[kBeamList];      // (score, place); in step 3 the logit's bits for the score
     __shared__ int2 s_piece[kBeamPieceList];
@@ -516,33 +546,48 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
             if (s_sum64[k] != 1) continue;
             if (tid == 0) s_total[0] = s_total[1] = s_total[2] = 0ull;
             __syncthreads();
-            add_exponentials<THREADS == 256 ? 2 : THREADS == 512 && SIDE == 1 ? 4 : 1, THREADS>(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld, p.V, s_top[k], s_total);
+            add_exponentials<THREADS == 512 && SIDE == 1 ? 4 : 2, THREADS>(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld, p.V, s_top[k], s_total);
             __syncthreads();
             if (tid == 0) {
                 const double sum = (static_cast<double>(s_total[2]) * 0x1p64 + static_cast<double>(s_total[1]) * 0x1p32) + static_cast<double>(s_total[0]);
-                s_lse[k] = static_cast<double>(s_top[k]) + log(sum * 0x1p-62);
+                s_lse[k] = static_cast<double>(s_top[k]) + log(sum * 0x1p-52);
                 s_sum64[k] = 2;
             }
         }
         __syncthreads();
     };
-    // Ahead of a cut by scores: those of all rows that the floor leaves, unless that is a single one.
-    auto settle_rows = [&] {
-        const bool left = tid < p.K && (s_state[tid] == 2 || (s_state[tid] == 1 && within(tid, s_top[tid])));
-        if (__syncthreads_count(left) < 2) return;
-        if (left && s_sum64[tid] == 0) s_sum64[tid] = 1;
-        __syncthreads();
-        sum_again();
+    // block_cut, at scores of which those of different beams may be off: with all that may belong before the cut, if these are no more than
+    // `most`; otherwise once more, with the sums of all rows that the floor leaves in 64 bits.
+    const double reach = 2.0 * static_cast<double>(__uint_as_float(s_unsure));
+    auto sure_cut = [&](auto reaches, auto again, long long last_place, int cap, int most, unsigned long long& t, long long& limit) {
+#pragma unroll 1
+        for (bool sure = false;; sure = true) {
+            block_cut(reaches, 1ull, ~0ull, last_place, p.n, cap, t, limit);
+            const bool left = tid < p.K && (s_state[tid] == 2 || (s_state[tid] == 1 && within(tid, s_top[tid])));
+            if (__syncthreads_count(left) < 2 || sure) return;
+            const unsigned long long low = ordered_bits64(from_ordered_bits64(t) - reach);
+            if (reaches(low, last_place) <= most) {
+                t = low;
+                limit = last_place;
+                return;
+            }
+            if (left && s_sum64[tid] == 0) s_sum64[tid] = 1;
+            __syncthreads();
+            sum_again();
+            again();
+        }
     };
     const bool crowded = L > kBeamPieceList;
     if (crowded) {
         finish_lse();
         __syncthreads();
-        settle_rows();
         unsigned long long key[kBeamItems];
+        auto score_pieces = [&] {
 #pragma unroll
-        for (int j = 0; j < kBeamItems; ++j)
-            key[j] = top[TWO && j >= kHalf] > DISCO_NEG_INF && best[j] > DISCO_NEG_INF ? score_of(item_row(j), best[j]) : 0ull;
+            for (int j = 0; j < kBeamItems; ++j)
+                key[j] = top[TWO && j >= kHalf] > DISCO_NEG_INF && best[j] > DISCO_NEG_INF ? score_of(item_row(j), best[j]) : 0ull;
+        };
+        score_pieces();
         auto pieces_reach = [&](unsigned long long u, long long limit) {
             int c = 0;
 #pragma unroll
@@ -551,7 +596,7 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
         };
         unsigned long long t;
         long long limit;
-        block_cut(pieces_reach, 1ull, ~0ull, (long long)p.K * deal.pieces, p.n, 2 * p.n, t, limit);
+        sure_cut(pieces_reach, score_pieces, (long long)p.K * deal.pieces, 2 * p.n, kBeamPieceList, t, limit);
         if (tid == 0) s_pieces = 0;
         __syncthreads();
 #pragma unroll
@@ -628,7 +673,6 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
             else s_cand[i * THREADS + tid].x = x;
         }
     } else {      // many equal logits
-        settle_rows();
         auto each = [&](auto f) {
             for (int i = tid; i < values; i += THREADS) {
                 int k, v;
@@ -645,7 +689,7 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
         };
         unsigned long long t;
         long long limit;
-        block_cut(values_reach, 1ull, ~0ull, (long long)kBeamMaxBeams << 32, p.n, kBeamList, t, limit);
+        sure_cut(values_reach, [] {}, (long long)kBeamMaxBeams << 32, kBeamList / 2, kBeamList, t, limit);
         __syncthreads();
         if (tid == 0) s_count = 0;
         __syncthreads();
@@ -658,12 +702,12 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
     // ---- 4 ----
     N = min(s_count, kBeamList);      // (the same)
     const long long out = (long long)b * p.n;
-    const double reach = 2.0 * static_cast<double>(__uint_as_float(s_unsure));
-    // Candidates of another beam, no better than c, that may be better if the sums of exponentials are off.
-    auto near = [&](const ulonglong2& c, unsigned long long low, const ulonglong2& o) {
-        return static_cast<int>(o.x >= low) & static_cast<int>(o.x <= c.x) & static_cast<int>(o.y >> 32 != c.y >> 32);
-    };
+    // The key of the least score that may be better than c's if the sums of exponentials are off.
     auto low_of = [&](const ulonglong2& c) { return ordered_bits64(from_ordered_bits64(c.x) - reach); };
+    auto beam_of = [](const ulonglong2& c) { return static_cast<int>(c.y >> 32); };
+    auto close_to = [&](const ulonglong2& c, unsigned long long low, const ulonglong2& o) {
+        return static_cast<int>(o.x >= low) & static_cast<int>(o.x <= c.x) & static_cast<int>(beam_of(o) != beam_of(c));
+    };
     for (;;) {
         bool unsure = false;
         for (int i = tid; i < N; i += THREADS) {
@@ -674,10 +718,10 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
             for (int j = 0; j < N; ++j) {       // (no branches: with them a candidate costs 140 cycles)
                 const ulonglong2 o = s_cand[j];
                 rank += static_cast<int>(o.x > c.x) | (static_cast<int>(o.x == c.x) & static_cast<int>(o.y < c.y));
-                close |= near(c, low, o);
+                close |= close_to(c, low, o);
             }
             if (rank < p.n) {       // (what is read of the beams has been read: the outputs may take the inputs' place)
-                const int parent = static_cast<int>(c.y >> 32), token = static_cast<int>(c.y & 0xffffffffull);
+                const int parent = beam_of(c), token = static_cast<int>(c.y & 0xffffffffull);
                 p.score_out[out + rank] = static_cast<float>(from_ordered_bits64(c.x));
                 p.parent[out + rank] = parent;
                 p.token[out + rank] = token;
@@ -691,11 +735,12 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
         for (int i = tid; i < N; i += THREADS) {
             const ulonglong2 c = s_cand[i];
             const unsigned long long low = low_of(c);
-            const int k = static_cast<int>(c.y >> 32);
+            const int k = beam_of(c);
+#pragma unroll 4
             for (int j = 0; j < N; ++j) {
                 const ulonglong2 o = s_cand[j];
-                const int l = static_cast<int>(o.y >> 32);
-                if (!near(c, low, o) || (s_sum64[k] == 2 && s_sum64[l] == 2)) continue;
+                const int l = beam_of(o);
+                if (!close_to(c, low, o) || (s_sum64[k] == 2 && s_sum64[l] == 2)) continue;
                 if (s_sum64[k] == 0) s_sum64[k] = 1;
                 if (s_sum64[l] == 0) s_sum64[l] = 1;
                 more = true;
@@ -704,9 +749,8 @@ __global__ void __launch_bounds__(THREADS, SIDE) beam_select_kernel(const BeamPa
         if (!__syncthreads_or(more)) break;
         sum_again();
         for (int i = tid; i < N; i += THREADS) {
-            const unsigned long long place = s_cand[i].y;
-            const int k = static_cast<int>(place >> 32);
-            if (s_state[k] == 1) s_cand[i].x = score_of(k, logit(k, static_cast<int>(place & 0xffffffffull)));
+            const int k = beam_of(s_cand[i]);
+            if (s_state[k] == 1) s_cand[i].x = score_of(k, logit(k, static_cast<int>(s_cand[i].y & 0xffffffffull)));
         }
         __syncthreads();
     }
