@@ -22,7 +22,6 @@ constexpr int kBeamStatWarps = 8;
 constexpr int kBeamThreads = 1024;       // of the selection, at most
 constexpr int kBeamCluster = 8;          // CTAs that make the pass over a sequence's logits and select, in one launch
 constexpr int kBeamItems = 8;            // pieces of rows that a thread of it holds
-constexpr int kBeamMaxKept = DISCO_MAX_KEPT;
 constexpr int kBeamMaxBeams = DISCO_MAX_BEAMS;
 constexpr int kBeamList = 1024;          // candidates that are ranked by counting
 constexpr int kBeamPieceList = 512;      // pieces that are looked into
@@ -43,7 +42,8 @@ struct BeamDeal {
         return d;
     }
     // Warps: as few of 8, 16 and 32 as hold every chunk as a piece of its own, otherwise 32; more where many are kept, since step 3 reads
-    // about as many pieces.
+    // about as many pieces.  (us a pass of 64 x 4 of 32000, 4 / 10 / 16 / 24 / 32 kept, 8 warps 14.0 / 15.8 / 17.9 / 21.1 / 24.8, 16 warps 14.1 /
+    // 14.8 / 15.9 / 17.4 / 18.9, 32 warps 15.2 / 15.6 / 16.0 / 17.0 / 17.7; of 500 x 2 of 8000, 2 / 10 kept, 17.6 / 23.8, 19.2 / 23.2, 31.0 / 34.0.)
     __host__ __device__ static int warps(int K, int chunks, int n) {
         for (int w = n <= 10 ? 8 : n <= 24 ? 16 : 32; w < 32; w *= 2)
             if (K <= w && make(K, chunks, w).merged == 1) return w;
@@ -52,8 +52,8 @@ struct BeamDeal {
 };
 
 // The pass over the logits and the selection in one launch: where a cluster has a warp for each segment of a sequence's logits, and the
-// clusters fit side by side.  (us a pass, two launches -> one: 1 / 4 / 16 / 64 x 4 beams of 32000 fp32 logits 14.0 / 10.4 / 11.1 / 14.8 -> 8.9 /
-// 9.5 / 10.4 / 15.4; with two segments to a warp and more, 20 x 5 of 40011 bf16 13.6 -> 14.9, 1 x 16 of 49152 fp32 11.3 -> 16.7.)
+// clusters fit side by side.  (us a pass, two launches -> one: 1 / 4 / 16 / 32 / 64 x 4 beams of 32000 fp32 logits 13.5 / 9.7 / 9.8 / 10.7 / 14.1 ->
+// 8.4 / 8.8 / 10.0 / 12.2 / 17.7; with two segments to a warp and more, 20 x 5 of 40011 bf16 12.5 -> 14.7, 1 x 16 of 49152 fp32 11.2 -> 16.3.)
 __host__ __device__ inline bool beam_joined(int B, int K, int segs) { return B <= 32 && K * segs <= 16 * kBeamCluster; }
 
 // How far the logarithm of a row's sum of exponentials in fp32 may be off: relatively, the sum.  In units of 2^-24, for N terms a record, S
@@ -301,6 +301,7 @@ __device__ __forceinline__ void add_exponentials(const T* z, int V, float top, u
 // SIDE: CTAs that are to fit an SM side by side.
 template <typename T, int CHUNK, int THREADS, bool TWO, bool JOINED, int SIDE = 1>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_select_kernel(const BeamParams p) {
+    static_assert(THREADS <= kBeamThreads && kBeamMaxBeams <= THREADS && DISCO_MAX_KEPT <= THREADS, "a thread to a beam, and to a place");
     constexpr int kWarps = THREADS / 32;
     __shared__ ulonglong2 s_cand[kBeamList];      // (score, place); in step 3 the logit's bits for the score
     __shared__ int2 s_piece[kBeamPieceList];
@@ -396,7 +397,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
             if constexpr (CHUNK != kBeamChunk) {
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
-                            const float now = warp_max_nan_f32(top[r]);
+                    const float now = warp_max_nan_f32(top[r]);
                     if (now > m[r]) e[r] *= __expf(m[r] - now);
                     m[r] = now;
 #pragma unroll
@@ -409,7 +410,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
         if constexpr (CHUNK == kBeamChunk) {
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
-                    const float now = warp_max_nan_f32(max_nan(m[r], top[r]));
+                const float now = warp_max_nan_f32(max_nan(m[r], top[r]));
                 e[r] = m[r] > DISCO_NEG_INF ? e[r] * __expf(m[r] - now) : 0.f;
                 m[r] = now;
             }
@@ -463,7 +464,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
     }
     auto high = [&](int r, float z) { return (z + offset[r]) + (err[r] + 0x1p-21f * fabsf(z)); };      // the most that a logit may score
     // The n-th largest of the threads' bounds, or a little less.  Each step costs a barrier that counts, so the search goes out from the
-    // largest one, in strides that grow until n reach it, and only then halves what is left.
+    // largest one, in strides that grow until n reach it, and only then halves what is left, until 1.5 n at most do (n / 1.5 n / 2 n, us a pass: 20
+    // x 5, 10 kept, 13.8 / 12.4 / 12.9, 16 x 8, 32 kept, 14.6 / 14.0 / 16.3, 16 x 16, 40 kept, 19.7 / 21.2 / 21.8).
     auto find_floor = [&](float low, int use) {
         const uint32_t key = ordered_bits(low), top = __reduce_max_sync(kFullMask, key);
         if (lane == 0) atomicMax(&s_best[use], top);
@@ -509,7 +511,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
                 note_piece(item_row(j), item_piece(j) * width, best[j]);
     }
     __syncthreads();
-    const int few = 2 * p.n + 8;      // more than this are worth another search
+    const int few = 2 * p.n + 8;      // more than this are worth another search (n + 8 / 2 n + 8 / 4 n + 8: 16 x 8, 32 kept, 16.4 / 14.0 / 13.9, 16 x 16, 40 kept, 21.5 / 21.2 / 23.5)
     int L = s_pieces, turn = 0;
     if (L > few && L <= kBeamPieceList) {
         constexpr int kEach = (kBeamPieceList + THREADS - 1) / THREADS;

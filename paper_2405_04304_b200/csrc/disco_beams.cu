@@ -55,7 +55,7 @@ int launch_quantize(disco_ctx* c, QuantParams p, cudaStream_t st) {
     void (*kern)(QuantParams);
     int threads = kQuantThreads, ctas = p.rows;
     if (p.rows >= 2048) {
-        // A head: a warp to a narrow row, four to a wide one (32000 x 768 / 40011 x 1000 / 32000 x 5120: 19 / 28 / 105 us; four warps to a narrow
+        // A head: a warp to a narrow row, four to a wide one (32000 x 768 / 40011 x 1000 / 32000 x 5120: 20 / 30 / 105 us; four warps to a narrow
         // row 34 / 45, sixteen to a wide one 171).
         if (p.d <= 2048) ctas = (p.rows + 3) / 4;
         kern = p.d <= 1024   ? quantize_rows_kernel<T, 4, 1>
@@ -71,8 +71,9 @@ int launch_quantize(disco_ctx* c, QuantParams p, cudaStream_t st) {
                : p.d <= 4096 ? quantize_rows_kernel<T, 2, 8>
                : p.d <= 8192 ? quantize_rows_kernel<T, 2, 16>
                              : quantize_rows_kernel<T, 4, 16>;
-        // Many of them would be read behind the head's first tiles, which the product's CTAs request as soon as they may start (704 rows 108.7 ->
-        // 105.3 us; 11 / 256 rows 30.0 / 45.0 -> 30.3 / 46.4).
+        // Many of them would be read behind the head's first tiles, which the product's CTAs request as soon as they may start (us a pass of 256 /
+        // 320 / 384 / 448 / 512 / 600 / 704 rows of 32000 x 5120, early -> late: 44.8 / 57.8 / 67.3 / 73.4 / 80.7 / 97.5 / 111.1 -> 44.9 / 57.6 / 65.5 /
+        // 68.5 / 80.6 / 98.4 / 109.9).
         p.late = p.rows >= 512;
     }
     const cudaError_t e = launch_after(c, kern, dim3((unsigned)ctas), dim3((unsigned)threads), 0, st, p);

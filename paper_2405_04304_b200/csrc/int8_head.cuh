@@ -233,14 +233,14 @@ struct Int8Tiling {
         t.x_box = ctas == 2 ? t.N / 2 : (round_up(R, 8) < t.N ? round_up(R, 8) : t.N);
         return t;
     }
-    // The kind, from passes of 11 to 704 rows of heads of 8000 x 2048 to 49152 x 2048 and 32000 x 5120 (us, one / two / pair):
-    //   * up to 32 hidden rows the epilogue is short and HBM is the bound: two (32000 x 5120, 11 rows 31.2 / 30.3 / 31.4)
-    //   * beyond, it pays to have it under the next item's products: one (32000 x 768, 64 / 200 / 300 rows 10.0 / 15.0 / 16.9, 12.0 / 17.2 /
-    //     18.1, 12.4 / 17.4 / 20.8)
-    //   * long contractions of many rows are bound by the operands' way from L2: pair (32000 x 5120, 128 / 200 / 256 / 320 rows 36.8 / 45.1 /
-    //     53.4 / 63.0, 36.7 / 45.0 / 52.8 / 60.9, 36.1 / 42.3 / 48.7 / 59.2)
+    // The kind, from passes of 11 to 320 rows of heads of 8000 x 2048 to 49152 x 2048 and 32000 x 5120 (us, one / two / pair):
+    //   * up to 32 hidden rows the epilogue is short and HBM is the bound: two (32000 x 5120, 11 rows 30.6 / 30.3 / 32.8)
+    //   * beyond, it pays to have it under the next item's products: one (32000 x 768, 64 / 200 / 300 rows 9.0 / 13.8 / 16.7, 9.0 / 15.3 / 17.8,
+    //     10.9 / 15.5 / 21.1)
+    //   * long contractions of many rows are bound by the operands' way from L2: pair (32000 x 5120, 128 / 200 / 256 / 320 rows 35.8 / 41.2 /
+    //     51.8 / 63.3, 35.2 / 41.2 / 49.8 / 59.0, 35.2 / 42.3 / 47.4 / 55.1)
     // unless it leaves a CTA more vocabulary rows, rounds counted, by over 15 % (200 rows of 20000 x 3000: 2 x 96 for one and pair, 160 for
-    // two: 26.7 / 22.8 / 24.5).
+    // two: 27.2 / 24.1 / 24.6).
     __host__ __device__ int share() const { return rounds * w_box; }
     __host__ __device__ static Int8Tiling choose(int R, int V, int d, int grid) {
         const Int8Tiling two = make(R, V, grid, kI8Two);
@@ -277,9 +277,8 @@ struct Int8Ring {
     }
     // Hidden rows that the kernel rounds itself, in every CTA (its epilogue's warps have nothing else to do meanwhile), rather than a kernel
     // before it: where a lane can hold its part of them, and there are few enough that their loads do not wait behind the head's.  (us a pass,
-    // a kernel before -> in the kernel: 1 / 4 / 16 rows of 32000 x 768 9.4 / 9.4 / 9.4 -> 7.8 / 7.0 / 8.3; 1 / 4 / 8 / 16 of 32000 x 2048 15.4 /
-    // 15.7 / 16.0 / 16.6 -> 14.6 / 15.3 / 17.1 / 19.2; 1 / 4 of 32000 x 5120 29.9 / 30.2 -> 30.1 / 31.8; 1 / 8 of 49152 x 1024 12.0 / 12.3 ->
-    // 11.7 / 12.5.)
+    // a kernel before -> in the kernel: 1 / 4 / 16 rows of 32000 x 768 9.2 / 9.2 / 9.2 -> 7.6 / 6.9 / 9.0; 1 / 4 / 8 of 32000 x 2048 15.6 / 15.7 /
+    // 15.9 -> 14.3 / 14.9 / 16.9; 1 / 8 of 49152 x 1024 12.2 / 12.4 -> 11.7 / 12.4.)
     __host__ __device__ static bool few(int R, int V, int d) {
         if (R > kI8EpiWarps || d > 2048 || d > kI8EpiWarps / R * 256 * kI8FewChunks) return false;
         return R * d <= ((long long)V * d <= 32ll << 20 ? 16384 : 8192);
