@@ -25,6 +25,7 @@ constexpr int kBeamItems = 8;            // pieces of rows that a thread of it h
 constexpr int kBeamMaxBeams = DISCO_MAX_BEAMS;
 constexpr int kBeamList = 1024;          // candidates that are ranked by counting
 constexpr int kBeamPieceList = 512;      // pieces that are looked into
+constexpr int kBeamAhead = 4;            // their logits that a thread has on their way at once
 
 // How the chunks of a sequence's K rows are dealt to the warps of its CTA: a lane holds the largest logits of kBeamItems pieces, each of
 // `merged` neighbouring chunks of one row.  Up to as many beams as warps: `share` warps to a row; up to twice as many (of 32 warps): two
@@ -287,6 +288,300 @@ __device__ __forceinline__ void add_exponentials(const T* z, int V, float top, u
     }
 }
 
+// More candidates or pieces than this are worth another search for a floor.  (n + 8 / 2 n + 8 / 4 n + 8, us a pass: 16 x 8, 32 kept, 16.4 / 14.0 /
+// 13.9, 16 x 16, 40 kept, 21.5 / 21.2 / 23.5.)
+__device__ __forceinline__ int beam_few(int n) { return 2 * n + 8; }
+
+// What a CTA of the selection holds in shared memory.
+struct BeamShared {
+    ulonglong2 cand[kBeamList];      // (score, place); in step 3 the logit's bits for the score
+    int2 piece[kBeamPieceList];      // its row, its first token
+    float piece_top[kBeamPieceList];
+    double lse[kBeamMaxBeams];       // the sum of exponentials, then what is taken off a logit
+    float score[kBeamMaxBeams], top[kBeamMaxBeams], offset[kBeamMaxBeams], err[kBeamMaxBeams];
+    int state[kBeamMaxBeams];        // 0: no continuation, 1: expands, 2: finished
+    int sum64[kBeamMaxBeams];        // the row's sum of exponentials is 0: one of fp32, 1: to be one of 64 bits, 2: that, or none
+    unsigned long long total[3];
+    int sum[2][32];
+    uint32_t unsure;                 // how far a score may be off for its sum of exponentials, by the bits
+    int pieces, count;
+};
+
+// Steps of the selection that its quick way and its thorough one share.
+template <typename T, int CHUNK, int THREADS>
+struct BeamCta {
+    const BeamParams& p;
+    BeamShared& s;
+    int b;
+    float floor;      // no less than this do the n best score
+
+    __device__ __forceinline__ int width() const { return p.deal.merged * CHUNK; }
+    // May a logit's score reach the floor?
+    __device__ __forceinline__ bool within(int k, float z) const {
+        return z > DISCO_NEG_INF && !((z + s.offset[k]) + (s.err[k] + 0x1p-21f * fabsf(z)) < floor);
+    }
+    __device__ __forceinline__ unsigned long long score_of(int k, float z) const {
+        return ordered_bits64(static_cast<double>(s.score[k]) + (static_cast<double>(z) - s.lse[k]));
+    }
+    __device__ __forceinline__ void finish_lse() const {
+        for (int k = threadIdx.x; k < p.K; k += THREADS) s.lse[k] = static_cast<double>(s.top[k]) + log(s.lse[k]);
+    }
+    __device__ __forceinline__ const T* row(int k) const { return static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld; }
+    __device__ __forceinline__ void note_piece(int k, int v, float z) const {
+        const int at = atomicAdd(&s.pieces, 1);
+        if (at < kBeamPieceList) s.piece[at] = make_int2(k, v), s.piece_top[at] = z;
+    }
+    // Value i of the pieces.
+    __device__ __forceinline__ bool locate(int i, int& k, int& v) const {
+        const int l = p.deal.merged == 1 ? i / CHUNK : i / width();
+        const int2 piece = s.piece[l];
+        k = piece.x;
+        v = piece.y + (i - l * width());
+        return v < p.V;
+    }
+    // Values i0, i0 + THREADS, ... of the pieces; -inf where there is none.
+    __device__ __forceinline__ void load(int i0, int values, float (&z)[kBeamAhead], int (&k)[kBeamAhead], int (&v)[kBeamAhead]) const {
+#pragma unroll
+        for (int a = 0; a < kBeamAhead; ++a) {
+            const int i = i0 + a * THREADS;
+            z[a] = i < values && locate(i, k[a], v[a]) ? load_logit(row(k[a]) + v[a]) : DISCO_NEG_INF;
+        }
+    }
+    static __device__ __forceinline__ unsigned long long place_of(int k, int v) { return (unsigned long long)k << 32 | (unsigned int)v; }
+    static __device__ __forceinline__ int beam_of(const ulonglong2& c) { return static_cast<int>(c.y >> 32); }
+    __device__ __forceinline__ void take(unsigned long long x, unsigned long long place) const {
+        const int at = atomicAdd(&s.count, 1);
+        if (at < kBeamList) s.cand[at] = make_ulonglong2(x, place);
+    }
+    // How near scores of different beams may come before their order is in doubt.
+    __device__ __forceinline__ double reach() const { return 2.0 * static_cast<double>(__uint_as_float(s.unsure)); }
+    // The key of the least score that may be better than c's if the sums of exponentials are off.
+    static __device__ __forceinline__ unsigned long long low_of(const ulonglong2& c, double reach) {
+        return ordered_bits64(from_ordered_bits64(c.x) - reach);
+    }
+    static __device__ __forceinline__ int close_to(const ulonglong2& c, unsigned long long low, const ulonglong2& o) {
+        return static_cast<int>(o.x >= low) & static_cast<int>(o.x <= c.x) & static_cast<int>(beam_of(o) != beam_of(c));
+    }
+    // Ranks of the N candidates, by counting, and what is returned.  Is one of this thread's in doubt?
+    __device__ __forceinline__ bool rank(int N) const {
+        const long long out = (long long)b * p.n;
+        const double r = reach();
+        bool unsure = false;
+        for (int i = threadIdx.x; i < N; i += THREADS) {
+            const ulonglong2 c = s.cand[i];
+            const unsigned long long low = low_of(c, r);
+            int rank = 0, close = 0;
+#pragma unroll 4
+            for (int j = 0; j < N; ++j) {       // (no branches: with them a candidate costs 140 cycles)
+                const ulonglong2 o = s.cand[j];
+                rank += static_cast<int>(o.x > c.x) | (static_cast<int>(o.x == c.x) & static_cast<int>(o.y < c.y));
+                close |= close_to(c, low, o);
+            }
+            if (rank < p.n) {       // (what is read of the beams has been read: the outputs may take the inputs' place)
+                const int parent = beam_of(c), token = static_cast<int>(c.y & 0xffffffffull);
+                p.score_out[out + rank] = static_cast<float>(from_ordered_bits64(c.x));
+                p.parent[out + rank] = parent;
+                p.token[out + rank] = token;
+                if (p.finished_out) p.finished_out[out + rank] = token == p.eos || s.state[parent] == 2;
+                unsure = unsure || close != 0;
+            }
+        }
+        return unsure;
+    }
+    // Places that no continuation is left for.
+    __device__ __forceinline__ void no_more(int N) const {
+        const long long out = (long long)b * p.n;
+        for (int i = N + threadIdx.x; i < p.n; i += THREADS) {
+            p.score_out[out + i] = DISCO_NEG_INF;
+            p.parent[out + i] = -1;
+            p.token[out + i] = -1;
+            if (p.finished_out) p.finished_out[out + i] = 0;
+        }
+    }
+};
+
+// The selection from where its quick way does not lead on, for all threads of a CTA behind a barrier: with more pieces than the list holds (and
+// sums of exponentials that are not logarithms yet), more candidates, or candidates of different beams whose order is in doubt.  A function
+// of its own, called last of all: among the rest its code and its registers cost every call 2 - 4 us where the kernel's code is not in a cache.
+enum BeamDoubt { kBeamPieces, kBeamValues, kBeamOrder };
+template <typename T, int CHUNK, int THREADS, int SIDE>
+__device__ __noinline__ void beam_settle(const BeamParams& p, BeamShared& s, int b, float floor, BeamDoubt doubt) {
+    constexpr int kWarps = THREADS / 32;
+    BeamCta<T, CHUNK, THREADS> cta{p, s, b, floor};
+    const int tid = threadIdx.x;
+    const BeamDeal& deal = p.deal;
+    const double reach = cta.reach();
+    int turn = 0;
+    // The sums of exponentials that are to be of 64 bits (all threads, behind a barrier).
+    auto sum_again = [&] {
+#pragma unroll 1
+        for (int k = 0; k < p.K; ++k) {
+            if (s.sum64[k] != 1) continue;
+            if (tid == 0) s.total[0] = s.total[1] = s.total[2] = 0ull;
+            __syncthreads();
+            add_exponentials<THREADS == 512 && SIDE == 1 ? 4 : 2, THREADS>(cta.row(k), p.V, s.top[k], s.total);
+            __syncthreads();
+            if (tid == 0) {
+                const double sum = (static_cast<double>(s.total[2]) * 0x1p64 + static_cast<double>(s.total[1]) * 0x1p32) + static_cast<double>(s.total[0]);
+                s.lse[k] = static_cast<double>(s.top[k]) + log(sum * 0x1p-52);
+                s.sum64[k] = 2;
+            }
+        }
+        __syncthreads();
+    };
+    // block_cut, at scores of which those of different beams may be off: with all that may belong before the cut, if these are no more than
+    // `most`; otherwise once more, with the sums of all rows that the floor leaves in 64 bits.
+    auto sure_cut = [&](auto reaches, auto again, long long last_place, int cap, int most, unsigned long long& t, long long& limit) {
+#pragma unroll 1
+        for (bool sure = false;; sure = true) {
+            block_cut(reaches, 1ull, ~0ull, last_place, p.n, cap, t, limit);
+            const bool left = tid < p.K && (s.state[tid] == 2 || (s.state[tid] == 1 && cta.within(tid, s.top[tid])));
+            if (__syncthreads_count(left) < 2 || sure) return;
+            const unsigned long long low = ordered_bits64(from_ordered_bits64(t) - reach);
+            if (reaches(low, last_place) <= most) {
+                t = low;
+                limit = last_place;
+                return;
+            }
+            if (left && s.sum64[tid] == 0) s.sum64[tid] = 1;
+            __syncthreads();
+            sum_again();
+            again();
+        }
+    };
+    int L = min(s.pieces, kBeamPieceList);
+    auto each = [&](auto f) {      // the candidates: (score, place)
+        const int values = L * cta.width();
+#pragma unroll 1
+        for (int i0 = tid; i0 < values; i0 += kBeamAhead * THREADS) {
+            float z[kBeamAhead];
+            int k[kBeamAhead], v[kBeamAhead];
+            cta.load(i0, values, z, k, v);
+#pragma unroll
+            for (int a = 0; a < kBeamAhead; ++a)
+                if (z[a] > DISCO_NEG_INF && cta.within(k[a], z[a])) f(cta.score_of(k[a], z[a]), static_cast<long long>(cta.place_of(k[a], v[a])));
+        }
+        if (tid < p.K && s.state[tid] == 2) f(ordered_bits64(s.score[tid]), static_cast<long long>(cta.place_of(tid, p.eos)));
+    };
+    if (doubt == kBeamPieces) {
+        cta.finish_lse();
+        __syncthreads();
+        // (as many pieces as threads hold items of)
+        float best[kBeamItems];
+        unsigned long long key[kBeamItems];
+        const int all = p.K * deal.pieces;
+#pragma unroll
+        for (int j = 0; j < kBeamItems; ++j) {
+            best[j] = DISCO_NEG_INF;
+            const int i = j * THREADS + tid, k = i / deal.pieces, first = (i - k * deal.pieces) * deal.merged;
+            if (i >= all || s.state[k] != 1) continue;
+            const long long at = (long long)(b * p.K + k) * p.chunks;
+            for (int c = first; c < min(first + deal.merged, p.chunks); ++c) {
+                if constexpr (CHUNK == kBeamChunk) best[j] = fmaxf(best[j], __ldcg(p.tops + at + c));
+                else best[j] = fmaxf(best[j], __ldcg(p.pairs + at + c).x);
+            }
+        }
+        auto score_pieces = [&] {
+#pragma unroll
+            for (int j = 0; j < kBeamItems; ++j) key[j] = best[j] > DISCO_NEG_INF ? cta.score_of((j * THREADS + tid) / deal.pieces, best[j]) : 0ull;
+        };
+        score_pieces();
+        auto pieces_reach = [&](unsigned long long u, long long limit) {
+            int c = 0;
+#pragma unroll
+            for (int j = 0; j < kBeamItems; ++j) c += key[j] > u || (key[j] == u && j * THREADS + tid <= limit);
+            return block_sum<kWarps>(c, s.sum, turn);
+        };
+        unsigned long long t;
+        long long limit;
+        sure_cut(pieces_reach, score_pieces, all, 2 * p.n, kBeamPieceList, t, limit);
+        if (tid == 0) s.pieces = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kBeamItems; ++j) {
+            const int i = j * THREADS + tid, k = i / deal.pieces;
+            if (key[j] > t || (key[j] == t && i <= limit)) cta.note_piece(k, (i - k * deal.pieces) * cta.width(), best[j]);
+        }
+        // (more pieces than the list holds, so n at least have been found)
+        cta.floor = __double2float_rd(from_ordered_bits64(t));
+        __syncthreads();
+        L = min(s.pieces, kBeamPieceList);      // (a matter of course, unless the statistics are those of a product whose wait ran out)
+        each([&](unsigned long long x, long long place) { cta.take(x, place); });
+        __syncthreads();
+        if (s.count > kBeamList) doubt = kBeamValues;
+    }
+    if (doubt == kBeamValues) {      // many equal logits
+        auto values_reach = [&](unsigned long long u, long long limit) {
+            int c = 0;
+            each([&](unsigned long long x, long long place) { c += x > u || (x == u && place <= limit); });
+            return block_sum<kWarps>(c, s.sum, turn);
+        };
+        unsigned long long t;
+        long long limit;
+        sure_cut(values_reach, [] {}, (long long)kBeamMaxBeams << 32, kBeamList / 2, kBeamList, t, limit);
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        each([&](unsigned long long x, long long place) {
+            if (x > t || (x == t && place <= limit)) cta.take(x, place);
+        });
+        __syncthreads();
+    }
+    int N = min(s.count, kBeamList);
+    auto score_again = [&] {
+        for (int i = tid; i < N; i += THREADS) {
+            const int k = cta.beam_of(s.cand[i]);
+            if (s.state[k] == 1) s.cand[i].x = cta.score_of(k, load_logit(cta.row(k) + static_cast<int>(s.cand[i].y & 0xffffffffull)));
+        }
+        __syncthreads();
+    };
+    if (doubt != kBeamOrder && N > beam_few(p.n)) {      // ranking takes as many steps as there are candidates
+        auto list_reach = [&](unsigned long long u, long long limit) {
+            int c = 0;
+            for (int i = tid; i < N; i += THREADS) c += s.cand[i].x > u || (s.cand[i].x == u && static_cast<long long>(s.cand[i].y) <= limit);
+            return block_sum<kWarps>(c, s.sum, turn);
+        };
+        unsigned long long t;
+        long long limit;
+        sure_cut(list_reach, score_again, (long long)kBeamMaxBeams << 32, beam_few(p.n), kBeamList, t, limit);
+        constexpr int kEach = (kBeamList + THREADS - 1) / THREADS;
+        ulonglong2 c[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) c[i] = i * THREADS + tid < N ? s.cand[i * THREADS + tid] : make_ulonglong2(0ull, ~0ull);
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (c[i].x > t || (c[i].x == t && static_cast<long long>(c[i].y) <= limit)) cta.take(c[i].x, c[i].y);
+        __syncthreads();
+        N = min(s.count, kBeamList);
+    }
+#pragma unroll 1
+    while (__syncthreads_or(cta.rank(N)) && p.K > 1) {
+        // Once more with sums of 64 bits of the beams that matter, if they are not of 64 bits already (so as many rounds as beams, at most).
+        bool more = false;
+        for (int i = tid; i < N; i += THREADS) {
+            const ulonglong2 c = s.cand[i];
+            const unsigned long long low = cta.low_of(c, reach);
+            const int k = cta.beam_of(c);
+#pragma unroll 4
+            for (int j = 0; j < N; ++j) {
+                const ulonglong2 o = s.cand[j];
+                const int l = cta.beam_of(o);
+                if (!cta.close_to(c, low, o) || (s.sum64[k] == 2 && s.sum64[l] == 2)) continue;
+                if (s.sum64[k] == 0) s.sum64[k] = 1;
+                if (s.sum64[l] == 0) s.sum64[l] = 1;
+                more = true;
+            }
+        }
+        if (!__syncthreads_or(more)) break;
+        sum_again();
+        score_again();
+    }
+    cta.no_more(N);
+}
+
 // A CTA to a sequence.  JOINED: a cluster of CTAs, which first of all make the pass over the sequence's logits; one of them goes on.
 //   1  each row's soft-max statistics from its chunks'
 //   2  the pieces that may hold the n best: every piece is known by its best score.  The n-th largest of what the threads have at best is
@@ -297,25 +592,16 @@ __device__ __forceinline__ void add_exponentials(const T* z, int V, float top, u
 //      of the sequences, of 8 of 8 below 0.1 %.  A beam's sum takes 9 - 19 us, of 32000 logits by 512 threads - of 49152 by 256.)
 // Up to 4 everything is in fp32 with a bound on its error, from which a piece or a logit is dropped only if it cannot be among the n best:
 // the 64-bit units are too few for a score for every piece (of 32000 logits and 4 beams, 8400 and 4400 cycles for steps 1 and 2 in 64 bits).
-// Where too many are equal for the lists (a call that is full of ties), the cuts are made in 64 bits, by bisection.
+// Where too many are equal for the lists (a call that is full of ties), the cuts are made in 64 bits, by bisection (beam_settle, like the
+// sums of 64 bits).
 // SIDE: CTAs that are to fit an SM side by side.
 template <typename T, int CHUNK, int THREADS, bool TWO, bool JOINED, int SIDE = 1>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_select_kernel(const BeamParams p) {
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_select_kernel(const __grid_constant__ BeamParams p) {
     static_assert(THREADS <= kBeamThreads && kBeamMaxBeams <= THREADS && DISCO_MAX_KEPT <= THREADS, "a thread to a beam, and to a place");
     constexpr int kWarps = THREADS / 32;
-    __shared__ ulonglong2 s_cand[kBeamList];      // (score, place); in step 3 the logit's bits for the score
-    __shared__ int2 s_piece[kBeamPieceList];
-    __shared__ float s_piece_top[kBeamPieceList];
-    __shared__ int s_sum[2][32];
+    __shared__ BeamShared s;
     __shared__ float s_max[2][32];
     __shared__ double s_exp[2][32];
-    __shared__ double s_lse[kBeamMaxBeams];     // the sum of exponentials, then what is taken off a logit
-    __shared__ float s_score[kBeamMaxBeams], s_top[kBeamMaxBeams], s_offset[kBeamMaxBeams], s_err[kBeamMaxBeams];
-    __shared__ int s_state[kBeamMaxBeams];      // 0: no continuation, 1: expands, 2: finished
-    __shared__ int s_sum64[kBeamMaxBeams];      // the row's sum of exponentials is 0: one of fp32, 1: to be one of 64 bits, 2: that, or none
-    __shared__ unsigned long long s_total[3];
-    __shared__ uint32_t s_unsure;               // how far a score may be off for its sum of exponentials, by the bits
-    __shared__ int s_pieces, s_count;
     __shared__ uint32_t s_best[3];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -334,7 +620,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
     auto item_row = [&](int j) { return TWO && j >= kHalf ? warp_row + 32 : warp_row; };
     auto item_piece = [&](int j) { return ((TWO ? j & (kHalf - 1) : j) * deal.share + warp_share) * 32 + lane; };
     auto item_used = [&](int j) { return (TWO ? j & (kHalf - 1) : j) < deal.used; };
-    auto piece_place = [&](int j) { return item_row(j) * deal.pieces + item_piece(j); };
 
     // ---- 1 ----
     float best[kBeamItems], top[kRows];      // the largest logits of this lane's pieces, and of those of a row
@@ -381,11 +666,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
                 if (tid < p.K) {
                     const float c = p.score[b * p.K + tid];
                     const bool over = p.finished && p.finished[b * p.K + tid];
-                    s_score[tid] = c;
-                    s_state[tid] = !beam_lives(c) ? 0 : over ? 2 : 1;
+                    s.score[tid] = c;
+                    s.state[tid] = !beam_lives(c) ? 0 : over ? 2 : 1;
                 }
                 if (tid < 3) s_best[tid] = 0u;
-                if (tid == 0) s_count = 0, s_pieces = 0, s_unsure = 0u;
+                if (tid == 0) s.count = 0, s.pieces = 0, s.unsure = 0u;
             }
 #pragma unroll
             for (int j = 0; j < kBeamItems; ++j) {
@@ -433,31 +718,31 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(kFullMask, sum, off);
         if (lane == 0) {
-            if (!is && s_state[k] == 1) s_state[k] = 0;
-            s_lse[k] = sum;
-            s_top[k] = top;
+            if (!is && s.state[k] == 1) s.state[k] = 0;
+            s.lse[k] = sum;
+            s.top[k] = top;
             // score = logit + offset, and what fp32 makes of that: a few roundings of numbers of these sizes and of the logarithm, and
             // the error of the sum, which the logarithm passes on whatever its size (the sum's own rounding to fp32, 2^-24, among it)
             const float ln = logf(static_cast<float>(sum));
-            s_offset[k] = s_score[k] - (top + ln);
-            s_err[k] = (0x1p-21f * fabsf(s_score[k]) + 0x1p-21f * fabsf(top)) + (0x1p-21f * ln + p.ln_err);
+            s.offset[k] = s.score[k] - (top + ln);
+            s.err[k] = (0x1p-21f * fabsf(s.score[k]) + 0x1p-21f * fabsf(top)) + (0x1p-21f * ln + p.ln_err);
             // (an offset beyond what fp32 holds says nothing of the scores: no bound, so nothing of the row is dropped)
-            if (!(fabsf(s_offset[k]) < -DISCO_NEG_INF)) s_err[k] = -DISCO_NEG_INF;
+            if (!(fabsf(s.offset[k]) < -DISCO_NEG_INF)) s.err[k] = -DISCO_NEG_INF;
         }
     }
     __syncthreads();
 
     // ---- 2 ----
-    if (tid < p.K) s_sum64[tid] = s_state[tid] == 1 ? 0 : 2;
+    if (tid < p.K) s.sum64[tid] = s.state[tid] == 1 ? 0 : 2;
     // (a warp's rows, the second one where it has two)
     float offset[kRows], err[kRows];
     float low = DISCO_NEG_INF;      // the least that the best of this thread's pieces may score
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
         const int k = warp_row + 32 * r;
-        const bool expands = k < p.K && s_state[k] == 1;
-        offset[r] = expands ? s_offset[k] : 0.f;
-        err[r] = expands ? s_err[k] : 0.f;
+        const bool expands = k < p.K && s.state[k] == 1;
+        offset[r] = expands ? s.offset[k] : 0.f;
+        err[r] = expands ? s.err[k] : 0.f;
         if (!expands) top[r] = DISCO_NEG_INF;       // (nothing of this row counts)
         const float f = top[r] + offset[r];
         if (top[r] > DISCO_NEG_INF && f < -DISCO_NEG_INF) low = fmaxf(low, f - (err[r] + 0x1p-21f * fabsf(top[r])));       // (beyond what fp32 holds: no bound)
@@ -489,30 +774,24 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
         }
         return lo > 0x007fffffu ? from_ordered_bits(lo) : DISCO_NEG_INF;
     };
-    float floor = find_floor(low, 0);
-    const int width = deal.merged * CHUNK;
-    auto note_piece = [&](int k, int v, float z) {      // its row, its first token, its largest logit
-        const int at = atomicAdd(&s_pieces, 1);
-        if (at < kBeamPieceList) s_piece[at] = make_int2(k, v), s_piece_top[at] = z;
-    };
-    auto within = [&](int k, float z) { return z > DISCO_NEG_INF && !((z + s_offset[k]) + (s_err[k] + 0x1p-21f * fabsf(z)) < floor); };
+    BeamCta<T, CHUNK, THREADS> cta{p, s, b, find_floor(low, 0)};
     auto bound = [&](int k, float z) {
-        const float f = z + s_offset[k];
-        return f < -DISCO_NEG_INF ? f - (s_err[k] + 0x1p-21f * fabsf(z)) : DISCO_NEG_INF;
+        const float f = z + s.offset[k];
+        return f < -DISCO_NEG_INF ? f - (s.err[k] + 0x1p-21f * fabsf(z)) : DISCO_NEG_INF;
     };
-    if (tid < p.K && s_state[tid] == 1 && within(tid, s_top[tid]))       // (and what 64 bits make of numbers of these sizes)
-        atomicMax(&s_unsure, __float_as_uint(p.ln_err + 0x1p-50f * (fabsf(s_score[tid]) + fabsf(s_top[tid]))));
+    if (tid < p.K && s.state[tid] == 1 && cta.within(tid, s.top[tid]))       // (and what 64 bits make of numbers of these sizes)
+        atomicMax(&s.unsure, __float_as_uint(p.ln_err + 0x1p-50f * (fabsf(s.score[tid]) + fabsf(s.top[tid]))));
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
-        if (!(top[r] > DISCO_NEG_INF) || high(r, top[r]) < floor) continue;      // (so it is with most threads)
+        if (!(top[r] > DISCO_NEG_INF) || high(r, top[r]) < cta.floor) continue;      // (so it is with most threads)
 #pragma unroll
         for (int j = 0; j < kBeamItems; ++j)
-            if (item_used(j) && (TWO && j >= kHalf) == (r == 1) && best[j] > DISCO_NEG_INF && !(high(r, best[j]) < floor))
-                note_piece(item_row(j), item_piece(j) * width, best[j]);
+            if (item_used(j) && (TWO && j >= kHalf) == (r == 1) && best[j] > DISCO_NEG_INF && !(high(r, best[j]) < cta.floor))
+                cta.note_piece(item_row(j), item_piece(j) * cta.width(), best[j]);
     }
     __syncthreads();
-    const int few = 2 * p.n + 8;      // more than this are worth another search (n + 8 / 2 n + 8 / 4 n + 8: 16 x 8, 32 kept, 16.4 / 14.0 / 13.9, 16 x 16, 40 kept, 21.5 / 21.2 / 23.5)
-    int L = s_pieces, turn = 0;
+    const int few = beam_few(p.n);
+    int L = s.pieces;
     if (L > few && L <= kBeamPieceList) {
         constexpr int kEach = (kBeamPieceList + THREADS - 1) / THREADS;
         int2 piece[kEach];
@@ -521,247 +800,78 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : SIDE) beam_selec
         for (int i = 0; i < kEach; ++i) {
             z[i] = DISCO_NEG_INF;
             if (i * THREADS + tid >= L) continue;
-            piece[i] = s_piece[i * THREADS + tid];
-            z[i] = s_piece_top[i * THREADS + tid];
+            piece[i] = s.piece[i * THREADS + tid];
+            z[i] = s.piece_top[i * THREADS + tid];
             low = fmaxf(low, bound(piece[i].x, z[i]));
         }
         const float next = find_floor(low, 1);
         __syncthreads();
-        if (tid == 0) s_pieces = 0;
-        floor = fmaxf(floor, next);
+        if (tid == 0) s.pieces = 0;
+        cta.floor = fmaxf(cta.floor, next);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (z[i] > DISCO_NEG_INF && within(piece[i].x, z[i])) note_piece(piece[i].x, piece[i].y, z[i]);
+            if (z[i] > DISCO_NEG_INF && cta.within(piece[i].x, z[i])) cta.note_piece(piece[i].x, piece[i].y, z[i]);
         __syncthreads();
-        L = s_pieces;
+        L = s.pieces;
     }
-    auto score_of = [&](int k, float z) { return ordered_bits64(static_cast<double>(s_score[k]) + (static_cast<double>(z) - s_lse[k])); };
-    auto finish_lse = [&] {
-        for (int k = tid; k < p.K; k += THREADS) s_lse[k] = static_cast<double>(s_top[k]) + log(s_lse[k]);
-    };
-    auto logit = [&](int k, int v) { return load_logit(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld + v); };
-    // The sums of exponentials that are to be of 64 bits (all threads, behind a barrier).
-    auto sum_again = [&] {
-#pragma unroll 1
-        for (int k = 0; k < p.K; ++k) {
-            if (s_sum64[k] != 1) continue;
-            if (tid == 0) s_total[0] = s_total[1] = s_total[2] = 0ull;
-            __syncthreads();
-            add_exponentials<THREADS == 512 && SIDE == 1 ? 4 : 2, THREADS>(static_cast<const T*>(p.z) + (long long)(b * p.K + k) * p.ld, p.V, s_top[k], s_total);
-            __syncthreads();
-            if (tid == 0) {
-                const double sum = (static_cast<double>(s_total[2]) * 0x1p64 + static_cast<double>(s_total[1]) * 0x1p32) + static_cast<double>(s_total[0]);
-                s_lse[k] = static_cast<double>(s_top[k]) + log(sum * 0x1p-52);
-                s_sum64[k] = 2;
-            }
-        }
-        __syncthreads();
-    };
-    // block_cut, at scores of which those of different beams may be off: with all that may belong before the cut, if these are no more than
-    // `most`; otherwise once more, with the sums of all rows that the floor leaves in 64 bits.
-    const double reach = 2.0 * static_cast<double>(__uint_as_float(s_unsure));
-    auto sure_cut = [&](auto reaches, auto again, long long last_place, int cap, int most, unsigned long long& t, long long& limit) {
-#pragma unroll 1
-        for (bool sure = false;; sure = true) {
-            block_cut(reaches, 1ull, ~0ull, last_place, p.n, cap, t, limit);
-            const bool left = tid < p.K && (s_state[tid] == 2 || (s_state[tid] == 1 && within(tid, s_top[tid])));
-            if (__syncthreads_count(left) < 2 || sure) return;
-            const unsigned long long low = ordered_bits64(from_ordered_bits64(t) - reach);
-            if (reaches(low, last_place) <= most) {
-                t = low;
-                limit = last_place;
-                return;
-            }
-            if (left && s_sum64[tid] == 0) s_sum64[tid] = 1;
-            __syncthreads();
-            sum_again();
-            again();
-        }
-    };
-    const bool crowded = L > kBeamPieceList;
-    if (crowded) {
-        finish_lse();
-        __syncthreads();
-        unsigned long long key[kBeamItems];
-        auto score_pieces = [&] {
-#pragma unroll
-            for (int j = 0; j < kBeamItems; ++j)
-                key[j] = top[TWO && j >= kHalf] > DISCO_NEG_INF && best[j] > DISCO_NEG_INF ? score_of(item_row(j), best[j]) : 0ull;
-        };
-        score_pieces();
-        auto pieces_reach = [&](unsigned long long u, long long limit) {
-            int c = 0;
-#pragma unroll
-            for (int j = 0; j < kBeamItems; ++j) c += key[j] > u || (key[j] == u && piece_place(j) <= limit);
-            return block_sum<kWarps>(c, s_sum, turn);
-        };
-        unsigned long long t;
-        long long limit;
-        sure_cut(pieces_reach, score_pieces, (long long)p.K * deal.pieces, 2 * p.n, kBeamPieceList, t, limit);
-        if (tid == 0) s_pieces = 0;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kBeamItems; ++j)
-            if (key[j] > t || (key[j] == t && piece_place(j) <= limit)) note_piece(item_row(j), item_piece(j) * width, best[j]);
-        // (more pieces than the list holds, so n at least have been found)
-        floor = __double2float_rd(from_ordered_bits64(t));
-        __syncthreads();
-        L = min(s_pieces, kBeamPieceList);      // (a matter of course, unless the statistics are those of a product whose wait ran out)
-    }
+    if (L > kBeamPieceList) return beam_settle<T, CHUNK, THREADS, SIDE>(p, s, b, cta.floor, kBeamPieces);
 
     // ---- 3 ----
-    const int values = L * width;
-    auto locate = [&](int i, int& k, int& v) {      // value i of the pieces
-        const int l = deal.merged == 1 ? i / CHUNK : i / width;
-        const int2 piece = s_piece[l];
-        k = piece.x;
-        v = piece.y + (i - l * width);
-        return v < p.V;
-    };
-    auto place_of = [&](int k, int v) { return (unsigned long long)k << 32 | (unsigned int)v; };
-    auto take = [&](unsigned long long x, unsigned long long place) {
-        const int at = atomicAdd(&s_count, 1);
-        if (at < kBeamList) s_cand[at] = make_ulonglong2(x, place);
-    };
-    constexpr int kAhead = 4;
-    bool first = !crowded;
-    for (int i0 = tid; i0 - tid < values; i0 += kAhead * THREADS) {
-        float z[kAhead];
-        int k[kAhead], v[kAhead];
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            const int i = i0 + a * THREADS;
-            z[a] = i < values && locate(i, k[a], v[a]) ? logit(k[a], v[a]) : DISCO_NEG_INF;
-        }
-        if (first) finish_lse();       // (while the loads are on their way)
+    const int values = L * cta.width();
+    bool first = true;
+    for (int i0 = tid; i0 - tid < values; i0 += kBeamAhead * THREADS) {
+        float z[kBeamAhead];
+        int k[kBeamAhead], v[kBeamAhead];
+        cta.load(i0, values, z, k, v);
+        if (first) cta.finish_lse();       // (while the loads are on their way)
         first = false;
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a)       // (a logit stands in for its score, which step 4 needs)
-            if (z[a] > DISCO_NEG_INF && within(k[a], z[a])) take(__float_as_uint(z[a]), place_of(k[a], v[a]));
+        for (int a = 0; a < kBeamAhead; ++a)       // (a logit stands in for its score, which step 4 needs)
+            if (z[a] > DISCO_NEG_INF && cta.within(k[a], z[a])) cta.take(__float_as_uint(z[a]), cta.place_of(k[a], v[a]));
     }
-    if (first) finish_lse();
-    if (tid < p.K && s_state[tid] == 2) take(0ull, place_of(tid, p.eos));
+    if (first) cta.finish_lse();
+    if (tid < p.K && s.state[tid] == 2) cta.take(0ull, cta.place_of(tid, p.eos));
     __syncthreads();
-    int N = s_count;
-    if (N <= kBeamList) {
+    int N = s.count;
+    if (N > kBeamList) return beam_settle<T, CHUNK, THREADS, SIDE>(p, s, b, cta.floor, kBeamValues);
+    {
         constexpr int kEach = (kBeamList + THREADS - 1) / THREADS;
         ulonglong2 cand[kEach];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) cand[i] = i * THREADS + tid < N ? s_cand[i * THREADS + tid] : make_ulonglong2(0ull, ~0ull);
-        auto row_of = [](const ulonglong2& c) { return static_cast<int>(c.y >> 32); };
+        for (int i = 0; i < kEach; ++i) cand[i] = i * THREADS + tid < N ? s.cand[i * THREADS + tid] : make_ulonglong2(0ull, ~0ull);
         auto logit_of = [](const ulonglong2& c) { return __uint_as_float(static_cast<uint32_t>(c.x)); };
         if (N > few) {
             float low = DISCO_NEG_INF;
 #pragma unroll
             for (int i = 0; i < kEach; ++i)
-                if (cand[i].y != ~0ull && s_state[row_of(cand[i])] == 1) low = fmaxf(low, bound(row_of(cand[i]), logit_of(cand[i])));
-            floor = fmaxf(floor, find_floor(low, 2));
+                if (cand[i].y != ~0ull && s.state[cta.beam_of(cand[i])] == 1) low = fmaxf(low, bound(cta.beam_of(cand[i]), logit_of(cand[i])));
+            cta.floor = fmaxf(cta.floor, find_floor(low, 2));
         }
         const bool again = N > few;
         if (again) {
             __syncthreads();
-            if (tid == 0) s_count = 0;
+            if (tid == 0) s.count = 0;
             __syncthreads();
         }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             if (cand[i].y == ~0ull) continue;
-            const int k = row_of(cand[i]);
-            const bool ended = s_state[k] == 2;
-            if (again && !ended && !within(k, logit_of(cand[i]))) continue;
-            const unsigned long long x = ended ? ordered_bits64(s_score[k]) : score_of(k, logit_of(cand[i]));
-            if (again) take(x, cand[i].y);
-            else s_cand[i * THREADS + tid].x = x;
+            const int k = cta.beam_of(cand[i]);
+            const bool ended = s.state[k] == 2;
+            if (again && !ended && !cta.within(k, logit_of(cand[i]))) continue;
+            const unsigned long long x = ended ? ordered_bits64(s.score[k]) : cta.score_of(k, logit_of(cand[i]));
+            if (again) cta.take(x, cand[i].y);
+            else s.cand[i * THREADS + tid].x = x;
         }
-    } else {      // many equal logits
-        auto each = [&](auto f) {
-            for (int i = tid; i < values; i += THREADS) {
-                int k, v;
-                if (!locate(i, k, v)) continue;
-                const float z = logit(k, v);
-                if (z > DISCO_NEG_INF && within(k, z)) f(score_of(k, z), static_cast<long long>(place_of(k, v)));
-            }
-            if (tid < p.K && s_state[tid] == 2) f(ordered_bits64(s_score[tid]), static_cast<long long>(place_of(tid, p.eos)));
-        };
-        auto values_reach = [&](unsigned long long u, long long limit) {
-            int c = 0;
-            each([&](unsigned long long x, long long place) { c += x > u || (x == u && place <= limit); });
-            return block_sum<kWarps>(c, s_sum, turn);
-        };
-        unsigned long long t;
-        long long limit;
-        sure_cut(values_reach, [] {}, (long long)kBeamMaxBeams << 32, kBeamList / 2, kBeamList, t, limit);
-        __syncthreads();
-        if (tid == 0) s_count = 0;
-        __syncthreads();
-        each([&](unsigned long long x, long long place) {
-            if (x > t || (x == t && place <= limit)) take(x, place);
-        });
     }
     __syncthreads();
 
     // ---- 4 ----
-    N = min(s_count, kBeamList);      // (the same)
-    const long long out = (long long)b * p.n;
-    // The key of the least score that may be better than c's if the sums of exponentials are off.
-    auto low_of = [&](const ulonglong2& c) { return ordered_bits64(from_ordered_bits64(c.x) - reach); };
-    auto beam_of = [](const ulonglong2& c) { return static_cast<int>(c.y >> 32); };
-    auto close_to = [&](const ulonglong2& c, unsigned long long low, const ulonglong2& o) {
-        return static_cast<int>(o.x >= low) & static_cast<int>(o.x <= c.x) & static_cast<int>(beam_of(o) != beam_of(c));
-    };
-    for (;;) {
-        bool unsure = false;
-        for (int i = tid; i < N; i += THREADS) {
-            const ulonglong2 c = s_cand[i];
-            const unsigned long long low = low_of(c);
-            int rank = 0, close = 0;
-#pragma unroll 4
-            for (int j = 0; j < N; ++j) {       // (no branches: with them a candidate costs 140 cycles)
-                const ulonglong2 o = s_cand[j];
-                rank += static_cast<int>(o.x > c.x) | (static_cast<int>(o.x == c.x) & static_cast<int>(o.y < c.y));
-                close |= close_to(c, low, o);
-            }
-            if (rank < p.n) {       // (what is read of the beams has been read: the outputs may take the inputs' place)
-                const int parent = beam_of(c), token = static_cast<int>(c.y & 0xffffffffull);
-                p.score_out[out + rank] = static_cast<float>(from_ordered_bits64(c.x));
-                p.parent[out + rank] = parent;
-                p.token[out + rank] = token;
-                if (p.finished_out) p.finished_out[out + rank] = token == p.eos || s_state[parent] == 2;
-                unsure = unsure || close != 0;
-            }
-        }
-        if (p.K == 1 || !__syncthreads_or(unsure)) break;
-        // Once more with sums of 64 bits of the beams that matter, if they are not of 64 bits already (so as many rounds as beams, at most).
-        bool more = false;
-        for (int i = tid; i < N; i += THREADS) {
-            const ulonglong2 c = s_cand[i];
-            const unsigned long long low = low_of(c);
-            const int k = beam_of(c);
-#pragma unroll 4
-            for (int j = 0; j < N; ++j) {
-                const ulonglong2 o = s_cand[j];
-                const int l = beam_of(o);
-                if (!close_to(c, low, o) || (s_sum64[k] == 2 && s_sum64[l] == 2)) continue;
-                if (s_sum64[k] == 0) s_sum64[k] = 1;
-                if (s_sum64[l] == 0) s_sum64[l] = 1;
-                more = true;
-            }
-        }
-        if (!__syncthreads_or(more)) break;
-        sum_again();
-        for (int i = tid; i < N; i += THREADS) {
-            const int k = beam_of(s_cand[i]);
-            if (s_state[k] == 1) s_cand[i].x = score_of(k, logit(k, static_cast<int>(s_cand[i].y & 0xffffffffull)));
-        }
-        __syncthreads();
-    }
-    for (int i = N + tid; i < p.n; i += THREADS) {
-        p.score_out[out + i] = DISCO_NEG_INF;
-        p.parent[out + i] = -1;
-        p.token[out + i] = -1;
-        if (p.finished_out) p.finished_out[out + i] = 0;
-    }
+    N = s.count;
+    const bool unsure = cta.rank(N);
+    cta.no_more(N);
+    if (p.K > 1 && __syncthreads_or(unsure)) beam_settle<T, CHUNK, THREADS, SIDE>(p, s, b, cta.floor, kBeamOrder);
 }
 
 // ---------------------------------------------------------------------------------------------

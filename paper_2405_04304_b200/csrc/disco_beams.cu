@@ -210,9 +210,9 @@ int launch_beam_select(disco_ctx* c, BeamParams p, cudaStream_t st) {
     p.deal = BeamDeal::make(p.K, p.chunks, warps);
     const int lanes = 32 * p.deal.share;
     p.ln_err = beam_ln_err(CHUNK == kBeamChunk ? (p.segs + lanes - 1) / lanes : p.deal.merged);
-    // Sixteen warps to a sequence: no register goes to memory where a CTA has an SM to itself (64 x 8 of 49152 28.2 -> 27.3 us a pass); two by two
-    // where there are more CTAs than SMs (160 x 4 on a head of 32000 x 768 48.7 -> 45.9) or, in clusters, half as many, since a GPC's SMs are no
-    // multiple of a cluster's CTAs (16 / 32 x 4 of 32000 11.1 / 14.8 -> 9.9 / 12.1; 8 x 4 the same).
+    // Sixteen warps to a sequence: no register goes to memory where a CTA has an SM to itself (us a pass, two by two -> one: 64 x 8 of 49152 27.6 ->
+    // 27.1, 20 x 5 of 40011 bf16 12.8 -> 12.0); two by two where there are more CTAs than SMs (160 x 4 on a head of 32000 x 768, one -> two 48.7 ->
+    // 45.4) or, in clusters, half as many, since a GPC's SMs are no multiple of a cluster's CTAs (16 / 32 x 4 of 32000 11.1 / 14.8 -> 9.8 / 11.9).
     const bool few = p.B * (JOINED ? 2 * kBeamCluster : 1) <= c->sm_count;
     auto kern = warps == 8    ? beam_select_kernel<T, CHUNK, 256, false, JOINED>
                 : warps == 16 ? (few ? beam_select_kernel<T, CHUNK, 512, false, JOINED> : beam_select_kernel<T, CHUNK, 512, false, JOINED, 2>)
